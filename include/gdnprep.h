@@ -83,6 +83,9 @@ enum {
                                 bf16 only (GDN_ERR_UNSUPPORTED with GDN_DTYPE_FP32) */
 };
 
+/* flags of gdn_layer_norm, gdn_layer_norm_backward */
+enum { GDN_NORM_RMS = 1 /* the mean is not subtracted: rows are divided by their root mean square */ };
+
 /* variants of the forward-substitution comparison kernel */
 enum { GDN_FWDSUBST_ROWS = 0, GDN_FWDSUBST_BLOCKED = 1, GDN_FWDSUBST_BLOCKED_TC = 2 };
 
@@ -313,6 +316,78 @@ int gdn_chunk_state_output_segmented_noalloc(const void* Q, const void* K, const
                                              float scale, const float* S_in, void* O_out, float* S_out, int segments,
                                              unsigned flags, gdn_stream_t stream);
 
+/*
+ * The gated delta rule token by token: decoding (the recurrence the chunk-wise layer evaluates, Sec. 2.1). For each of B sequences, its T new
+ * tokens in turn, with S the sequence's state, per value head, updated in place:
+ *     S <- exp(g_t) S;   u = beta_t (v_t - S k_t);   S <- S + u k_t^T;   o_t = scale S q_t
+ *   Q, K [B,H_k,T,d_k], V, O_out [B,H_v,T,d_v], beta, g [B,H_v,T] (g: raw log-gates, fp32), or token-major [B,T,H,d] and
+ *   [B,T,H_v] with GDN_FLAG_LAYOUT_BTHD. `dtype`: element type of Q, K, V, O. With GDN_FLAG_K_L2NORM the rows of K and Q are
+ *   L2-normalised here (a row of zeros stays zero).
+ *   S [n_slots,H_v,d_v,d_k], fp32 or bf16 (`state_dtype`): the layout of gdn_chunk_state_output's S_out. All arithmetic is fp32; a bf16
+ *   state is rounded once per call.
+ *   slots: DEVICE array of B int32, the state of each sequence, or NULL: sequence b has state b (n_slots >= B then). A negative slot
+ *   is a padded row of the batch: nothing of it is read, its output is zero. No slot may appear twice and none may reach n_slots:
+ *   of two sequences with the same slot the first in the batch is computed; the other, like one whose slot is out of range, gets the
+ *   output zero, changes no state, and gdn_device_status reports GDN_ERR_INVALID_ARG.
+ * Any T >= 0 (a long prompt is faster through gdn_gated_delta_layer), d_k and d_v up to 256 in multiples of 8.
+ */
+int gdn_recurrent_step(const void* Q, const void* K, const void* V, const float* beta, const float* g, int B, int H_k, int H_v, int T,
+                       int d_k, int d_v, float scale, int dtype, void* S, int state_dtype, const int32_t* slots, int n_slots,
+                       void* O_out, unsigned flags, gdn_stream_t stream);
+
+/*
+ * Backward pass of the chunk-wise layer (gdn_gated_delta_layer with raw log-gates): the gradients of a scalar loss L with
+ * respect to every input, given dO = dL/dO and dS_out = dL/dS_out. They are those of the gated delta rule itself (the exact inverse in each chunk;
+ * the forward pass' truncated series differs from it by less than its bf16 rounding).
+ *   dO, V, dV [B,H_v,T,d_v], Q, K, dQ, dK [B,H_k,T,d_k] bf16, beta, g, dbeta, dg [B,H_v,T] fp32 (g: raw log-gates), or
+ *   token-major with GDN_FLAG_LAYOUT_BTHD. Gradients of a key head shared by several value heads are summed in fp32.
+ *   With GDN_FLAG_K_L2NORM Q and K are the raw projections and dQ, dK their gradients, through the normalisation.
+ *   S_in, dS_out, dS_in [B,H_v,d_v,d_k] fp32, each may be NULL (zero state; no gradient; not wanted).
+ *   T: any length >= 0, a last chunk may be short (rows behind it are neither read nor written). flags: GDN_FLAG_G_RAW is required
+ *   (GDN_ERR_UNSUPPORTED without it), GDN_FLAG_LAYOUT_BTHD and GDN_FLAG_K_L2NORM are optional.
+ *   workspace: DEVICE memory of gdn_gated_delta_layer_backward_workspace(B, B * T, H_v) bytes (B = 0 or T = 0: none), 16-byte
+ *   aligned, owned by the caller and free to reuse when the stream has passed the call. It holds every chunk's state and its gradient; nothing
+ *   is kept from the forward pass. Calls that may overlap need a workspace each.
+ * The result does not depend on timing (no atomics). A log-gate below -128 counts as -128. dbeta, dg and dS_in are accurate to fp32
+ * arithmetic; dQ, dK, dV to their rounding to bf16.
+ * Supported: C = 64, d_k = d_v = 128.
+ */
+int gdn_gated_delta_layer_backward(const void* dO, const void* Q, const void* K, const void* V, const float* beta, const float* g, int B,
+                                   int H_k, int H_v, int T, int C, int d_k, int d_v, float scale, const float* S_in, const float* dS_out,
+                                   void* dQ, void* dK, void* dV, float* dbeta, float* dg, float* dS_in, void* workspace,
+                                   size_t workspace_bytes, unsigned flags, gdn_stream_t stream);
+
+/*
+ * The same for packed sequences (the tensors of gdn_chunk_state_output_varlen): sequence s holds the tokens [cu_seqlens[s], cu_seqlens[s + 1]) of
+ * tensors with T_total tokens; cu_seqlens: DEVICE array of n_seq + 1 int32, non-decreasing, 0 <= cu_seqlens[0],
+ * cu_seqlens[n_seq] <= T_total. S_in, dS_out, dS_in [n_seq,H_v,d_v,d_k]. Rows of the gradients that no sequence covers are left
+ * untouched. workspace: gdn_gated_delta_layer_backward_workspace(n_seq, T_total, H_v) bytes.
+ */
+int gdn_gated_delta_layer_backward_varlen(const void* dO, const void* Q, const void* K, const void* V, const float* beta, const float* g,
+                                          const int32_t* cu_seqlens, int n_seq, int T_total, int H_k, int H_v, int C, int d_k, int d_v,
+                                          float scale, const float* S_in, const float* dS_out, void* dQ, void* dK, void* dV,
+                                          float* dbeta, float* dg, float* dS_in, void* workspace, size_t workspace_bytes,
+                                          unsigned flags, gdn_stream_t stream);
+size_t gdn_gated_delta_layer_backward_workspace(int n_seq, long long tokens, int H_v);
+
+/*
+ * Row normalisation with weight, bias and SiLU gate: what the layer's output passes through before the output projection (rows
+ * of a head's d_v features, GDN_NORM_RMS, gated), and the layer norm of a model's blocks.
+ *     n = (x - mean(x)) / sqrt(var(x) + eps)      (GDN_NORM_RMS: n = x / sqrt(mean(x^2) + eps))
+ *     y = (n * weight + bias) * gate * sigmoid(gate)
+ *   x, gate, y [rows,width], contiguous, fp32 or bf16 (`dtype`); weight, bias [width], fp32 or bf16 (`param_dtype`); weight, bias
+ *   and gate may each be NULL (1, 0, and no gate). y may be x or gate. 1 <= width <= 16384. Statistics and arithmetic in fp32.
+ * Backward: dx, dgate like x (dgate exactly where there is a gate), dweight, dbias [width] fp32: sums over the rows, accumulated in fp32 in an
+ *   order that depends on the shape alone; required where there is a weight / a bias, NULL otherwise. dx may be dy or x, dgate may be gate.
+ *   workspace: DEVICE memory of gdn_layer_norm_backward_workspace(rows, width) bytes, 16-byte aligned (needed for dweight or dbias).
+ */
+int gdn_layer_norm(const void* x, const void* weight, const void* bias, const void* gate, long long rows, int width, float eps, int dtype,
+                   int param_dtype, void* y, unsigned flags, gdn_stream_t stream);
+int gdn_layer_norm_backward(const void* dy, const void* x, const void* weight, const void* bias, const void* gate, long long rows, int width,
+                            float eps, int dtype, int param_dtype, void* dx, float* dweight, float* dbias, void* dgate,
+                            void* workspace, size_t workspace_bytes, unsigned flags, gdn_stream_t stream);
+size_t gdn_layer_norm_backward_workspace(long long rows, int width);
+
 /* Checksum of the 256-entry gate-decay table round(2^15 * 2^(-f/256)) the INT8 kernel uses
  * (sum_f: s = (31 s + table[f] + f) mod 1000000007), so that a CPU evaluation can confirm it holds the same table. */
 unsigned int gdn_int8_lut_checksum(void);
@@ -320,7 +395,8 @@ unsigned int gdn_int8_lut_checksum(void);
 /*
  * Waits for `stream`, then returns and clears the status word the kernels of
  * this library write on the current device: GDN_OK, or GDN_ERR_TIMEOUT when a
- * bounded wait inside a kernel gave up (its outputs are then undefined).
+ * bounded wait inside a kernel gave up (its outputs are then undefined), or
+ * GDN_ERR_INVALID_ARG when gdn_recurrent_step met a slot it cannot use.
  * This is the only call that synchronises.
  */
 int gdn_device_status(gdn_stream_t stream);

@@ -31,6 +31,7 @@ GDN_FLAG_K_L2NORM = 2
 GDN_FLAG_OUT_FP32 = 4
 GDN_FLAG_LAYOUT_BTHD = 8
 GDN_FLAG_W_GATED = 16
+GDN_NORM_RMS = 1
 GDN_FWDSUBST_ROWS = 0
 GDN_FWDSUBST_BLOCKED = 1
 GDN_FWDSUBST_BLOCKED_TC = 2
@@ -40,6 +41,8 @@ EXPORTS = (
     "gdn_chunk_prepare_fwdsubst",
     "gdn_chunk_prepare_int8", "gdn_chunk_prepare_int16", "gdn_chunk_state_output", "gdn_chunk_state_output_varlen", "gdn_chunk_state_output_segmented",
     "gdn_chunk_state_output_segmented_noalloc", "gdn_gated_delta_layer",
+    "gdn_recurrent_step", "gdn_gated_delta_layer_backward", "gdn_gated_delta_layer_backward_varlen",
+    "gdn_gated_delta_layer_backward_workspace", "gdn_layer_norm", "gdn_layer_norm_backward", "gdn_layer_norm_backward_workspace",
     "gdn_chunk_state_segments", "gdn_chunk_state_segmented_workspace", "gdn_selftest_bounded_wait",
     "gdn_int8_lut_checksum",
     "gdn_device_status", "gdn_default_order", "gdn_default_residual_steps",
@@ -90,6 +93,23 @@ def load_library() -> ctypes.CDLL:
     lib.gdn_gated_delta_layer.argtypes = [vp, vp, vp, vp, vp, ip, ip, ip, ip, ip, ip, ip, ctypes.c_float, vp, vp, vp, vp, vp,
                                           ctypes.c_uint, vp]
     lib.gdn_gated_delta_layer.restype = ip
+    fp, up, ll, sz = ctypes.c_float, ctypes.c_uint, ctypes.c_longlong, ctypes.c_size_t
+    lib.gdn_recurrent_step.argtypes = [vp, vp, vp, vp, vp, ip, ip, ip, ip, ip, ip, fp, ip, vp, ip, vp, ip, vp, up, vp]
+    lib.gdn_recurrent_step.restype = ip
+    lib.gdn_gated_delta_layer_backward.argtypes = [vp, vp, vp, vp, vp, vp, ip, ip, ip, ip, ip, ip, ip, fp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                                   vp, sz, up, vp]
+    lib.gdn_gated_delta_layer_backward.restype = ip
+    lib.gdn_gated_delta_layer_backward_varlen.argtypes = [vp, vp, vp, vp, vp, vp, vp, ip, ip, ip, ip, ip, ip, ip, fp, vp, vp, vp, vp, vp, vp,
+                                                          vp, vp, vp, sz, up, vp]
+    lib.gdn_gated_delta_layer_backward_varlen.restype = ip
+    lib.gdn_gated_delta_layer_backward_workspace.argtypes = [ip, ll, ip]
+    lib.gdn_gated_delta_layer_backward_workspace.restype = sz
+    lib.gdn_layer_norm.argtypes = [vp, vp, vp, vp, ll, ip, fp, ip, ip, vp, up, vp]
+    lib.gdn_layer_norm.restype = ip
+    lib.gdn_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, ll, ip, fp, ip, ip, vp, vp, vp, vp, vp, sz, up, vp]
+    lib.gdn_layer_norm_backward.restype = ip
+    lib.gdn_layer_norm_backward_workspace.argtypes = [ll, ip]
+    lib.gdn_layer_norm_backward_workspace.restype = sz
     lib.gdn_chunk_state_segments.argtypes = [ip]
     lib.gdn_chunk_state_segments.restype = ip
     lib.gdn_chunk_state_segmented_workspace.argtypes = [ip, ip]
@@ -548,6 +568,186 @@ def gated_delta_layer(Q, K, V, beta, g_raw, C=64, scale=None, S_in=None, *, cu_s
     if rc != GDN_OK:
         raise GdnError(rc, "gdn_gated_delta_layer")
     return O, S_out
+
+
+def _check_tensors(where, device, *tensors):
+    """Contiguous tensors of one CUDA device, the current one (the library launches there)."""
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or t.device != device:
+            raise ValueError(f"{where}: all tensors must live on one CUDA device (there is no CPU path)")
+        if not t.is_contiguous():
+            raise ValueError(f"{where}: all tensors must be contiguous")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: the tensors live on {device}, which is not the current device")
+
+
+def _check_shape(where, name, t, shape, *dtypes):
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{where}: {name} is {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
+
+
+_TOKEN_TYPES = (torch.bfloat16, torch.float32)
+
+
+def _layer_shapes(where, Q, K, V, beta, g, token_major, packed, *dtypes):
+    """Sizes (B, H_k, H_v, T, d_k, d_v) of a layer's tensors, after a check that they fit each other."""
+    dims = 3 if packed else 4
+    if V.dim() != dims or K.dim() != dims:
+        raise ValueError(f"{where}: Q, K, V have {dims} dimensions here")
+    if token_major:
+        lead, (H_k, d_k), (H_v, d_v) = tuple(V.shape[:-2]), K.shape[-2:], V.shape[-2:]
+        T = lead[-1]
+        key, val, gate = (*lead, H_k, d_k), (*lead, H_v, d_v), (*lead, H_v)
+    else:
+        lead, (H_k, T, d_k), (H_v, _, d_v) = tuple(V.shape[:-3]), K.shape[-3:], V.shape[-3:]
+        key, val, gate = (*lead, H_k, T, d_k), (*lead, H_v, T, d_v), (*lead, H_v, T)
+    for name, t, shape in (("Q", Q, key), ("K", K, key), ("V", V, val)):
+        _check_shape(where, name, t, shape, *dtypes)
+    if not Q.dtype == K.dtype == V.dtype:
+        raise TypeError(f"{where}: Q, K and V share a dtype")
+    for name, t in (("beta", beta), ("g_raw", g)):
+        _check_shape(where, name, t, gate, torch.float32)
+    return (1 if packed else V.shape[0]), H_k, H_v, T, d_k, d_v
+
+
+def gated_delta_step(Q, K, V, beta, g_raw, S, slots=None, scale=None, *, token_major=True, qk_l2norm=True, out=None):
+    """Decoding: the gated delta rule token by token on a pool of states S [n_slots,H_v,d_v,d_k] (fp32 or bf16; the layout of the layer's
+    S_out), updated in place. Q, K [B,T,H_k,d], V [B,T,H_v,d] (bf16 or fp32), beta, g_raw [B,T,H_v] (token_major) or the head-major
+    forms; T = 1 for ordinary decoding, more where several tokens of a sequence are known at once. slots: int32 CUDA tensor [B],
+    the state of each sequence (negative: a padded row, whose output is zero; no slot twice, see the header); None: sequence b has state b.
+    Returns O like V."""
+    where = "gated_delta_step"
+    B, H_k, H_v, T, d_k, d_v = _layer_shapes(where, Q, K, V, beta, g_raw, token_major, False, *_TOKEN_TYPES)
+    if S.dim() != 4:
+        raise ValueError(f"{where}: S is [n_slots,H_v,d_v,d_k]")
+    _check_shape(where, "S", S, (S.shape[0], H_v, d_v, d_k), *_TOKEN_TYPES)
+    _check_shape(where, "slots", slots, (B,), torch.int32)
+    _check_shape(where, "out", out, V.shape, V.dtype)
+    _check_tensors(where, V.device, Q, K, V, beta, g_raw, S, slots, out)
+    O = torch.empty_like(V) if out is None else out
+    flags = (GDN_FLAG_LAYOUT_BTHD if token_major else 0) | (GDN_FLAG_K_L2NORM if qk_l2norm else 0)
+    rc = load_library().gdn_recurrent_step(_ptr(Q), _ptr(K), _ptr(V), _ptr(beta), _ptr(g_raw), B, H_k, H_v, T, d_k, d_v,
+                                           d_k ** -0.5 if scale is None else scale, _dtype_code(V), _ptr(S), _dtype_code(S), _ptr(slots),
+                                           S.shape[0], _ptr(O), flags, _stream())
+    if rc != GDN_OK:
+        raise GdnError(rc, "gdn_recurrent_step")
+    return O
+
+
+def gated_delta_layer_backward(dO, Q, K, V, beta, g_raw, C=64, scale=None, S_in=None, dS_out=None, *, cu_seqlens=None, token_major=True,
+                               qk_l2norm=True, workspace=None):
+    """Gradients of `gated_delta_layer` with the same arguments: dO like V (the gradient of O) and, where the final states went
+    into the loss, dS_out [B or n_seq,H_v,d_v,d_k] fp32. Any T. bf16, C = 64, d = 128. Nothing has to be kept from the forward pass.
+    workspace: a uint8 CUDA tensor of gdn_gated_delta_layer_backward_workspace bytes to reuse between calls (default: allocated).
+    Returns (dQ, dK, dV, dbeta, dg_raw, dS_in), dS_in None without an S_in. Rows that no packed sequence covers get zeros."""
+    where = "gated_delta_layer_backward"
+    packed = cu_seqlens is not None
+    B, H_k, H_v, T, d_k, d_v = _layer_shapes(where, Q, K, V, beta, g_raw, token_major, packed, torch.bfloat16)
+    _check_shape(where, "dO", dO, V.shape, torch.bfloat16)
+    if packed:
+        bounds = [int(x) for x in cu_seqlens]
+        if not bounds or bounds[0] < 0 or bounds[-1] > T or any(b < a for a, b in zip(bounds[:-1], bounds[1:])):
+            raise ValueError(f"{where}: cu_seqlens must be non-decreasing, from 0 on and up to the number of tokens")
+        B = len(bounds) - 1
+    for name, t in (("S_in", S_in), ("dS_out", dS_out)):
+        _check_shape(where, name, t, (B, H_v, d_v, d_k), torch.float32)
+    _check_tensors(where, V.device, dO, Q, K, V, beta, g_raw, S_in, dS_out, workspace)
+    lib = load_library()
+    need = int(lib.gdn_gated_delta_layer_backward_workspace(B, T if packed else B * T, H_v))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=V.device)
+    have = workspace.numel() * workspace.element_size()
+    if packed:
+        dQ, dK, dV, dbeta, dg = (_rows_like(t.shape, t, bounds, T) for t in (Q, K, V, beta, g_raw))
+    else:
+        dQ, dK, dV, dbeta, dg = (torch.empty_like(t) for t in (Q, K, V, beta, g_raw))
+    dS_in = None if S_in is None else torch.empty_like(S_in)
+    flags = GDN_FLAG_G_RAW | (GDN_FLAG_LAYOUT_BTHD if token_major else 0) | (GDN_FLAG_K_L2NORM if qk_l2norm else 0)
+    scale = d_k ** -0.5 if scale is None else scale
+    inputs = [_ptr(t) for t in (dO, Q, K, V, beta, g_raw)]
+    outputs = [_ptr(t) for t in (S_in, dS_out, dQ, dK, dV, dbeta, dg, dS_in, workspace)]
+    if packed:
+        cu = _int32_table(bounds, V.device)
+        rc = lib.gdn_gated_delta_layer_backward_varlen(*inputs, _ptr(cu), B, T, H_k, H_v, C, d_k, d_v, scale, *outputs, have, flags, _stream())
+    else:
+        rc = lib.gdn_gated_delta_layer_backward(*inputs, B, H_k, H_v, T, C, d_k, d_v, scale, *outputs, have, flags, _stream())
+    if rc != GDN_OK:
+        raise GdnError(rc, "gdn_gated_delta_layer_backward" + ("_varlen" if packed else ""))
+    return dQ, dK, dV, dbeta, dg, dS_in
+
+
+def gdn_gated_delta_layer_backward_varlen(dO, Q, K, V, beta, g_raw, cu_seqlens, n_seq, T_total, H_k, H_v, C, d_k, d_v, scale, S_in, dS_out,
+                                          dQ, dK, dV, dbeta, dg, dS_in, workspace, flags, *, check=True):
+    """Raw call of the packed form (cu_seqlens: int32 CUDA tensor of n_seq + 1 boundaries); it can be captured in a CUDA graph."""
+    tensors = (dO, Q, K, V, beta, g_raw, cu_seqlens, S_in, dS_out, dQ, dK, dV, dbeta, dg, dS_in, workspace)
+    _check_tensors("gdn_gated_delta_layer_backward_varlen", V.device, *tensors)
+    if cu_seqlens is not None and cu_seqlens.dtype != torch.int32:
+        raise TypeError("cu_seqlens is an int32 tensor")
+    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = load_library().gdn_gated_delta_layer_backward_varlen(
+        *(_ptr(t) for t in tensors[:7]), n_seq, T_total, H_k, H_v, C, d_k, d_v, scale, *(_ptr(t) for t in tensors[7:]), have, flags, _stream())
+    if check and rc != GDN_OK:
+        raise GdnError(rc, "gdn_gated_delta_layer_backward_varlen")
+    return rc
+
+
+def gdn_gated_delta_layer_backward_workspace(n_seq: int, tokens: int, H_v: int) -> int:
+    """Bytes of workspace of a backward call on n_seq sequences with `tokens` tokens in all (packed: the tensors' tokens)."""
+    return int(load_library().gdn_gated_delta_layer_backward_workspace(n_seq, tokens, H_v))
+
+
+def _norm_shapes(where, x, weight, bias, gate):
+    if x.dim() < 1 or x.dtype not in _TOKEN_TYPES:
+        raise TypeError(f"{where}: x is a bf16 or fp32 tensor of at least one dimension")
+    width = x.shape[-1]
+    for name, t in (("weight", weight), ("bias", bias)):
+        _check_shape(where, name, t, (width,), *_TOKEN_TYPES)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError(f"{where}: weight and bias share a dtype")
+    _check_shape(where, "gate", gate, x.shape, x.dtype)
+    return (x.numel() // width if width else 0), width, _dtype_code(next((t for t in (weight, bias) if t is not None), x))
+
+
+def layer_norm(x, weight=None, bias=None, gate=None, *, rms=False, eps=1e-5, out=None):
+    """Rows (the last dimension) of x normalised, times weight, plus bias, times silu(gate). rms: without subtracting the mean (the layer's
+    output norm: rms=True and a gate). weight, bias [width] fp32 or bf16; gate like x; each may be None. Returns y like x."""
+    where = "layer_norm"
+    rows, width, params = _norm_shapes(where, x, weight, bias, gate)
+    _check_shape(where, "out", out, x.shape, x.dtype)
+    _check_tensors(where, x.device, x, weight, bias, gate, out)
+    y = torch.empty_like(x) if out is None else out
+    rc = load_library().gdn_layer_norm(_ptr(x), _ptr(weight), _ptr(bias), _ptr(gate), rows, width, eps, _dtype_code(x), params, _ptr(y),
+                                       GDN_NORM_RMS if rms else 0, _stream())
+    if rc != GDN_OK:
+        raise GdnError(rc, "gdn_layer_norm")
+    return y
+
+
+def layer_norm_backward(dy, x, weight=None, bias=None, gate=None, *, rms=False, eps=1e-5, workspace=None):
+    """Gradients of `layer_norm` with the same arguments. Returns (dx, dweight, dbias, dgate): dx, dgate like x, dweight and dbias fp32;
+    None where there is no such input."""
+    where = "layer_norm_backward"
+    rows, width, params = _norm_shapes(where, x, weight, bias, gate)
+    _check_shape(where, "dy", dy, x.shape, x.dtype)
+    _check_tensors(where, x.device, dy, x, weight, bias, gate, workspace)
+    lib = load_library()
+    dx = torch.empty_like(x)
+    dgate = None if gate is None else torch.empty_like(gate)
+    dweight, dbias = (None if t is None else torch.empty(width, dtype=torch.float32, device=x.device) for t in (weight, bias))
+    if workspace is None and (weight is not None or bias is not None):
+        workspace = torch.empty(int(lib.gdn_layer_norm_backward_workspace(rows, width)), dtype=torch.uint8, device=x.device)
+    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.gdn_layer_norm_backward(_ptr(dy), _ptr(x), _ptr(weight), _ptr(bias), _ptr(gate), rows, width, eps, _dtype_code(x), params, _ptr(dx),
+                                     _ptr(dweight), _ptr(dbias), _ptr(dgate), _ptr(workspace), have, GDN_NORM_RMS if rms else 0, _stream())
+    if rc != GDN_OK:
+        raise GdnError(rc, "gdn_layer_norm_backward")
+    return dx, dweight, dbias, dgate
 
 
 def gdn_selftest_bounded_wait() -> int:

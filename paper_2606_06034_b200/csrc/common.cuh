@@ -94,6 +94,47 @@ struct ProblemS {
     int out_from = 0;  // S_out holds the final states of the sequences from this one on
 };
 
+// The gated delta rule token by token
+struct ProblemStep {
+    const void *Q, *K, *V;
+    const float *beta, *g;
+    void* S;
+    const int* slots;  // may be null: sequence b's state is S[b]
+    void* O;
+    int B, H_k, H_v, T, d_k, d_v, n_slots;
+    float scale;
+    int dtype, state_dtype;
+    unsigned flags;
+};
+
+// The layer's backward pass
+struct ProblemB {
+    const void *dO, *Q, *K, *V;
+    const float *beta, *g;
+    const float *S_in, *dS_out;  // may be null (zeros)
+    void *dQ, *dK, *dV;
+    float *dbeta, *dg;
+    float* dS_in;           // may be null
+    const int* cu_seqlens;  // null: n_seq sequences of T tokens; else the boundaries of packed ones in tensors of T tokens
+    int n_seq, T, H_k, H_v;
+    float scale;
+    unsigned flags;
+    void* workspace;
+};
+
+// Row normalisation and its backward pass
+struct ProblemN {
+    const void *dy, *x, *weight, *bias, *gate;  // weight, bias, gate may be null
+    void *y, *dx, *dgate;
+    float *dweight, *dbias;
+    void* workspace;
+    long long rows;
+    int width;
+    float eps;
+    int dtype, param_dtype;
+    unsigned flags;
+};
+
 enum InverseMode { INV_NEUMANN = 0, INV_FWDSUBST_ROWS = 1, INV_FWDSUBST_BLOCKED = 2, INV_FWDSUBST_TC = 3 };
 
 // Launches a kernel that may be set up while the kernel before it in the stream still runs, if that one has allowed it
@@ -135,6 +176,11 @@ int launch_chunk_state_segmented_builtin(const ProblemS& q, int P, cudaStream_t 
 int chunk_state_auto_segments(long long H_v);
 int launch_tc_int8(const ProblemI8& p, cudaStream_t stream);
 int launch_tc_int16(const ProblemI16& p, cudaStream_t stream);
+int launch_recurrent_step(const ProblemStep& p, cudaStream_t stream);
+int launch_layer_backward(const ProblemB& p, cudaStream_t stream);
+size_t layer_backward_workspace(int n_seq, long long tokens, int H_v);
+int launch_layer_norm(const ProblemN& p, bool backward, cudaStream_t stream);
+size_t norm_workspace(long long rows, int width);
 void int8_decay_lut(uint16_t* out256);  // table of round(2^15 * 2^(-f/256))
 
 }  // namespace gdn

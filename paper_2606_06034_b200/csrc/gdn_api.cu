@@ -1,6 +1,7 @@
 // C-ABI entry points: argument validation, kernel selection, status word.
 #include <atomic>
 #include <cstdint>
+#include <initializer_list>
 
 #include "common.cuh"
 
@@ -302,6 +303,109 @@ int gdn_chunk_state_output_varlen(const void* Q, const void* K, const void* W_ga
     q.seq_start = cu_seqlens;
     q.seq_end = cu_seqlens + 1;
     return launch_chunk_state(q, static_cast<cudaStream_t>(stream));
+}
+
+int gdn_recurrent_step(const void* Q, const void* K, const void* V, const float* beta, const float* g, int B, int H_k, int H_v, int T,
+                       int d_k, int d_v, float scale, int dtype, void* S, int state_dtype, const int32_t* slots, int n_slots,
+                       void* O_out, unsigned flags, gdn_stream_t stream) {
+    if (flags & ~static_cast<unsigned>(GDN_FLAG_LAYOUT_BTHD | GDN_FLAG_K_L2NORM)) return GDN_ERR_INVALID_ARG;
+    if (Q == nullptr || K == nullptr || V == nullptr || beta == nullptr || g == nullptr || S == nullptr || O_out == nullptr) return GDN_ERR_NULL;
+    if (B < 0 || H_k <= 0 || H_v <= 0 || T < 0 || d_k <= 0 || d_v <= 0 || n_slots < 0) return GDN_ERR_INVALID_ARG;
+    if (H_v % H_k != 0 || (slots == nullptr && n_slots < B)) return GDN_ERR_INVALID_ARG;
+    for (const int t : {dtype, state_dtype})
+        if (t != GDN_DTYPE_FP32 && t != GDN_DTYPE_BF16) return GDN_ERR_INVALID_ARG;
+    if (d_k % 8 != 0 || d_v % 8 != 0 || d_k > 256 || d_v > 256) return GDN_ERR_UNSUPPORTED;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(beta) || !aligned16(g) || !aligned16(S) || !aligned16(O_out) || !aligned16(slots))
+        return GDN_ERR_ALIGN;
+    const int rc = check_arch();
+    if (rc != GDN_OK || B == 0 || T == 0) return rc;
+    return launch_recurrent_step(ProblemStep{Q, K, V, beta, g, S, slots, O_out, B, H_k, H_v, T, d_k, d_v, n_slots, scale, dtype, state_dtype, flags},
+                                 static_cast<cudaStream_t>(stream));
+}
+
+size_t gdn_gated_delta_layer_backward_workspace(int n_seq, long long tokens, int H_v) {
+    return n_seq > 0 && tokens > 0 && H_v > 0 ? layer_backward_workspace(n_seq, tokens, H_v) : 0;
+}
+
+static int layer_backward(const ProblemB& q, int C, int d_k, int d_v, long long tokens, size_t workspace_bytes, gdn_stream_t stream) {
+    if (q.flags & ~static_cast<unsigned>(GDN_FLAG_G_RAW | GDN_FLAG_LAYOUT_BTHD | GDN_FLAG_K_L2NORM)) return GDN_ERR_INVALID_ARG;
+    for (const void* x : {q.dO, q.Q, q.K, q.V, static_cast<const void*>(q.beta), static_cast<const void*>(q.g), static_cast<const void*>(q.dQ),
+                          static_cast<const void*>(q.dK), static_cast<const void*>(q.dV), static_cast<const void*>(q.dbeta), static_cast<const void*>(q.dg)})
+        if (x == nullptr) return GDN_ERR_NULL;
+    if (q.n_seq < 0 || q.T < 0 || q.H_k <= 0 || q.H_v <= 0 || C < 2 || d_k <= 0 || d_v <= 0 || q.H_v % q.H_k != 0) return GDN_ERR_INVALID_ARG;
+    if ((q.flags & GDN_FLAG_G_RAW) == 0 || C != 64 || d_k != 128 || d_v != 128) return GDN_ERR_UNSUPPORTED;
+    const size_t need = gdn_gated_delta_layer_backward_workspace(q.n_seq, tokens, q.H_v);
+    if (need > 0 && q.workspace == nullptr) return GDN_ERR_NULL;
+    if (workspace_bytes < need) return GDN_ERR_INVALID_ARG;
+    for (const void* x : {q.dO, q.Q, q.K, q.V, static_cast<const void*>(q.beta), static_cast<const void*>(q.g), static_cast<const void*>(q.S_in),
+                          static_cast<const void*>(q.dS_out), static_cast<const void*>(q.dQ), static_cast<const void*>(q.dK), static_cast<const void*>(q.dV),
+                          static_cast<const void*>(q.dbeta), static_cast<const void*>(q.dg), static_cast<const void*>(q.dS_in),
+                          static_cast<const void*>(q.workspace)})
+        if (!aligned16(x)) return GDN_ERR_ALIGN;
+    const int rc = check_arch();
+    return rc != GDN_OK || q.n_seq == 0 ? rc : launch_layer_backward(q, static_cast<cudaStream_t>(stream));
+}
+
+int gdn_gated_delta_layer_backward(const void* dO, const void* Q, const void* K, const void* V, const float* beta, const float* g, int B,
+                                   int H_k, int H_v, int T, int C, int d_k, int d_v, float scale, const float* S_in, const float* dS_out,
+                                   void* dQ, void* dK, void* dV, float* dbeta, float* dg, float* dS_in, void* workspace,
+                                   size_t workspace_bytes, unsigned flags, gdn_stream_t stream) {
+    const ProblemB q{dO, Q, K, V, beta, g, S_in, dS_out, dQ, dK, dV, dbeta, dg, dS_in, nullptr, B, T, H_k, H_v, scale, flags, workspace};
+    return layer_backward(q, C, d_k, d_v, static_cast<long long>(B) * T, workspace_bytes, stream);
+}
+
+int gdn_gated_delta_layer_backward_varlen(const void* dO, const void* Q, const void* K, const void* V, const float* beta, const float* g,
+                                          const int32_t* cu_seqlens, int n_seq, int T_total, int H_k, int H_v, int C, int d_k, int d_v,
+                                          float scale, const float* S_in, const float* dS_out, void* dQ, void* dK, void* dV,
+                                          float* dbeta, float* dg, float* dS_in, void* workspace, size_t workspace_bytes,
+                                          unsigned flags, gdn_stream_t stream) {
+    if (cu_seqlens == nullptr) return GDN_ERR_NULL;
+    const ProblemB q{dO, Q, K, V, beta, g, S_in, dS_out, dQ, dK, dV, dbeta, dg, dS_in, cu_seqlens, n_seq, T_total, H_k, H_v, scale, flags, workspace};
+    return layer_backward(q, C, d_k, d_v, T_total, workspace_bytes, stream);
+}
+
+size_t gdn_layer_norm_backward_workspace(long long rows, int width) {
+    return rows > 0 && width > 0 && width <= 16384 ? norm_workspace(rows, width) : 0;
+}
+
+static int layer_norm(const ProblemN& q, bool backward, size_t workspace_bytes, gdn_stream_t stream) {
+    if (q.flags & ~static_cast<unsigned>(GDN_NORM_RMS)) return GDN_ERR_INVALID_ARG;
+    if (q.x == nullptr || (backward ? q.dy == nullptr || q.dx == nullptr : q.y == nullptr)) return GDN_ERR_NULL;
+    if (backward && ((q.weight != nullptr) != (q.dweight != nullptr) || (q.bias != nullptr) != (q.dbias != nullptr) ||
+                     (q.gate != nullptr) != (q.dgate != nullptr)))
+        return GDN_ERR_NULL;
+    if (q.rows < 0 || q.width <= 0 || !(q.eps >= 0.f)) return GDN_ERR_INVALID_ARG;
+    for (const int t : {q.dtype, q.param_dtype})
+        if (t != GDN_DTYPE_FP32 && t != GDN_DTYPE_BF16) return GDN_ERR_INVALID_ARG;
+    if (q.width > 16384) return GDN_ERR_UNSUPPORTED;
+    if (backward && (q.dweight != nullptr || q.dbias != nullptr)) {
+        const size_t need = gdn_layer_norm_backward_workspace(q.rows, q.width);
+        if (need > 0 && q.workspace == nullptr) return GDN_ERR_NULL;
+        if (workspace_bytes < need) return GDN_ERR_INVALID_ARG;
+    }
+    for (const void* x : {q.dy, q.x, q.weight, q.bias, q.gate, static_cast<const void*>(q.y), static_cast<const void*>(q.dx), static_cast<const void*>(q.dgate),
+                          static_cast<const void*>(q.dweight), static_cast<const void*>(q.dbias), static_cast<const void*>(q.workspace)})
+        if (!aligned16(x)) return GDN_ERR_ALIGN;
+    const int rc = check_arch();
+    return rc != GDN_OK ? rc : launch_layer_norm(q, backward, static_cast<cudaStream_t>(stream));
+}
+
+int gdn_layer_norm(const void* x, const void* weight, const void* bias, const void* gate, long long rows, int width, float eps, int dtype,
+                   int param_dtype, void* y, unsigned flags, gdn_stream_t stream) {
+    ProblemN q{};
+    q.x = x, q.weight = weight, q.bias = bias, q.gate = gate, q.y = y;
+    q.rows = rows, q.width = width, q.eps = eps, q.dtype = dtype, q.param_dtype = param_dtype, q.flags = flags;
+    return layer_norm(q, false, 0, stream);
+}
+
+int gdn_layer_norm_backward(const void* dy, const void* x, const void* weight, const void* bias, const void* gate, long long rows, int width,
+                            float eps, int dtype, int param_dtype, void* dx, float* dweight, float* dbias, void* dgate,
+                            void* workspace, size_t workspace_bytes, unsigned flags, gdn_stream_t stream) {
+    ProblemN q{};
+    q.dy = dy, q.x = x, q.weight = weight, q.bias = bias, q.gate = gate;
+    q.dx = dx, q.dgate = dgate, q.dweight = dweight, q.dbias = dbias, q.workspace = workspace;
+    q.rows = rows, q.width = width, q.eps = eps, q.dtype = dtype, q.param_dtype = param_dtype, q.flags = flags;
+    return layer_norm(q, true, workspace_bytes, stream);
 }
 
 int gdn_selftest_bounded_wait(gdn_stream_t stream) {

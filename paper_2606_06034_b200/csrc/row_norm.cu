@@ -1,0 +1,397 @@
+// Row normalisation with weight, bias and SiLU gate, forward and backward: what follows the layer's output in a model (rows of a head's
+// features, RMS, gated) and the layer norm of its blocks (rows of the model's width, mean and variance).
+//
+//     n = (x - mean) rstd   (GDN_NORM_RMS: mean = 0),   h = n w + b,   y = h silu(z)
+//     dh = dy silu(z),  dz = dy h silu'(z),  dw = sum_rows dh n,  db = sum_rows dh,
+//     dn = dh w,        dx = rstd (dn - mean(dn) - n mean(dn n))         (GDN_NORM_RMS: without mean(dn))
+//
+// What bounds it: HBM; every input is read once and every output written once. A row stays in registers between its load and its
+// store: 8 elements (16 bytes of bf16) a thread and vector, TPR threads a row, NV vectors a thread. The statistics are taken from the
+// registers, the mean first and then the squared distances from it, so nothing cancels. The backward pass forms the statistics again from x, which
+// it has to read anyway, instead of reading stored ones. A CTA walks many rows, so that weight and bias are read once per CTA, and in the
+// backward pass their gradients stay in registers until the CTA's last row; the CTAs' sums are added by a second small launch in a fixed
+// order: the result does not depend on timing.
+#include "common.cuh"
+#include "sm100_ptx.cuh"
+
+namespace gdn {
+namespace {
+
+using namespace sm100;
+
+struct ParamsN {
+    const void *dy, *x, *weight, *bias, *gate;  // weight, bias, gate may be null
+    void *y, *dx, *dgate;
+    float* partial;  // backward: [CTAs][2][width], sums of dw and db
+    long long rows;
+    int width;
+    float eps, inv_width;
+    bool rms, param_bf16, want_db;
+};
+
+// 8 elements of a row, as they are stored
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 w;
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        x[0] = bf16_lo(w.x), x[1] = bf16_hi(w.x), x[2] = bf16_lo(w.y), x[3] = bf16_hi(w.y);
+        x[4] = bf16_lo(w.z), x[5] = bf16_hi(w.z), x[6] = bf16_lo(w.w), x[7] = bf16_hi(w.w);
+    }
+    __device__ __forceinline__ void set(const float (&x)[8]) {
+        w = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+    }
+};
+template <>
+struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+    __device__ __forceinline__ void set(const float (&x)[8]) {
+        a = make_float4(x[0], x[1], x[2], x[3]), b = make_float4(x[4], x[5], x[6], x[7]);
+    }
+};
+__device__ __forceinline__ float one(const float* p) { return *p; }
+__device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// Vector `col .. col + 7` of a row that starts at `row`; elements past the width are zeros. VEC: width a multiple of 8, so every
+// vector is whole and aligned; else element by element.
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw8<T> load8(const T* row, int col, int width, bool active) {
+    Raw8<T> r;
+    if (VEC) {
+        if (active && col < width) {
+            r = *reinterpret_cast<const Raw8<T>*>(row + col);
+        } else {
+            const float zero[8] = {};
+            r.set(zero);
+        }
+    } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = active && col + e < width ? one(row + col + e) : 0.f;
+        r.set(x);
+    }
+    return r;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* row, int col, int width, bool active, const float (&x)[8]) {
+    if (VEC) {
+        if (active && col < width) {
+            Raw8<T> r;
+            r.set(x);
+            *reinterpret_cast<Raw8<T>*>(row + col) = r;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (active && col + e < width) put(row + col + e, x[e]);
+    }
+}
+// 8 elements of weight or bias (fp32 or bf16), `none` where there is no such tensor
+__device__ __forceinline__ void load_param(const void* p, bool bf16, int col, int width, float none, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        x[e] = p == nullptr || col + e >= width ? none
+               : bf16 ? one(static_cast<const __nv_bfloat16*>(p) + col + e) : one(static_cast<const float*>(p) + col + e);
+}
+
+// Sums of two values over the TPR threads of a row. TPR > 32 (the whole CTA): through `box`, of which two calls in a row use
+// different halves, so that one barrier a call is enough.
+template <int TPR>
+__device__ __forceinline__ void row_sums(float& a, float& b, float2* box, int& turn) {
+#pragma unroll
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    if (TPR > 32) {
+        constexpr int W = TPR / 32;
+        float2* const half = box + turn * W;
+        turn ^= 1;
+        if (threadIdx.x % 32 == 0) half[threadIdx.x / 32] = make_float2(a, b);
+        __syncthreads();
+        a = b = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) a += half[i].x, b += half[i].y;
+    }
+}
+
+// sigmoid; exp(-z) = inf gives 0
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+
+constexpr int kNormThreads = 256;
+template <int TPR>
+__host__ __device__ constexpr int cta_threads() { return TPR > kNormThreads ? TPR : kNormThreads; }
+
+template <typename T, int NV, int TPR>
+__device__ __forceinline__ void statistics(const Raw8<T> (&raw)[NV], int t, const ParamsN& p, float2* box, int& turn, float& mean, float& rstd) {
+    float s = 0.f, unused = 0.f;
+    mean = 0.f;
+    if (!p.rms) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float x[8];
+            raw[v].get(x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += x[e];
+        }
+        row_sums<TPR>(s, unused, box, turn);
+        mean = s * p.inv_width;
+    }
+    float q = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        float x[8];
+        raw[v].get(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = (v * TPR + t) * 8 + e < p.width ? x[e] - mean : 0.f;
+            q = fmaf(d, d, q);
+        }
+    }
+    row_sums<TPR>(q, unused, box, turn);
+    rstd = rsqrtf(q * p.inv_width + p.eps);
+}
+
+template <typename T, int NV, int TPR, bool VEC>
+__global__ void __launch_bounds__(cta_threads<TPR>()) norm_forward_kernel(const ParamsN p) {
+    constexpr int G = cta_threads<TPR>() / TPR;  // rows that a CTA has at a time
+    __shared__ float2 box[2 * (TPR > 32 ? TPR / 32 : 1)];
+    const int t = threadIdx.x % TPR;
+    int turn = 0;
+    float w[NV][8], b[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        load_param(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w[v]);
+        load_param(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, b[v]);
+    }
+    for (long long first = static_cast<long long>(blockIdx.x) * G; first < p.rows; first += static_cast<long long>(gridDim.x) * G) {
+        const long long row = first + threadIdx.x / TPR;
+        const bool active = row < p.rows;
+        const long long at = (active ? row : 0) * p.width;
+        Raw8<T> raw[NV], gate[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) raw[v] = load8<T, VEC>(static_cast<const T*>(p.x) + at, (v * TPR + t) * 8, p.width, active);
+        if (p.gate != nullptr) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) gate[v] = load8<T, VEC>(static_cast<const T*>(p.gate) + at, (v * TPR + t) * 8, p.width, active);
+        }
+        float mean, rstd;
+        statistics<T, NV, TPR>(raw, t, p, box, turn, mean, rstd);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float x[8], z[8];
+            raw[v].get(x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = fmaf((x[e] - mean) * rstd, w[v][e], b[v][e]);
+            if (p.gate != nullptr) {
+                gate[v].get(z);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= z[e] * sigmoid(z[e]);
+            }
+            store8<T, VEC>(static_cast<T*>(p.y) + at, (v * TPR + t) * 8, p.width, active, x);
+        }
+    }
+}
+
+template <typename T, int NV, int TPR, bool VEC>
+__global__ void __launch_bounds__(cta_threads<TPR>()) norm_backward_kernel(const ParamsN p) {
+    constexpr int G = cta_threads<TPR>() / TPR;
+    constexpr int kColumns = NV * TPR * 8;
+    __shared__ float2 box[2 * (TPR > 32 ? TPR / 32 : 1)];
+    __shared__ float gather[G > 1 ? G * kColumns : 1];
+    const int t = threadIdx.x % TPR;
+    int turn = 0;
+    float w[NV][8], b[NV][8], dw[NV][8] = {}, db[NV][8] = {};
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        load_param(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w[v]);
+        load_param(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, b[v]);
+    }
+    for (long long first = static_cast<long long>(blockIdx.x) * G; first < p.rows; first += static_cast<long long>(gridDim.x) * G) {
+        const long long row = first + threadIdx.x / TPR;
+        const bool active = row < p.rows;
+        const long long at = (active ? row : 0) * p.width;
+        Raw8<T> raw[NV], gate[NV], up[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            raw[v] = load8<T, VEC>(static_cast<const T*>(p.x) + at, (v * TPR + t) * 8, p.width, active);
+            up[v] = load8<T, VEC>(static_cast<const T*>(p.dy) + at, (v * TPR + t) * 8, p.width, active);
+        }
+        if (p.gate != nullptr) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) gate[v] = load8<T, VEC>(static_cast<const T*>(p.gate) + at, (v * TPR + t) * 8, p.width, active);
+        }
+        float mean, rstd;
+        statistics<T, NV, TPR>(raw, t, p, box, turn, mean, rstd);
+        // dh, its sums, the gate's gradient. Elements past the width have dy = 0 and so count for nothing.
+        float dh[NV][8], c0 = 0.f, c1 = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float x[8], z[8], dz[8];
+            raw[v].get(x);
+            up[v].get(dh[v]);
+            if (p.gate != nullptr) {
+                gate[v].get(z);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float s = sigmoid(z[e]), n = (x[e] - mean) * rstd;
+                    dz[e] = dh[v][e] * fmaf(n, w[v][e], b[v][e]) * s * fmaf(z[e], 1.f - s, 1.f);
+                    dh[v][e] *= z[e] * s;
+                }
+                store8<T, VEC>(static_cast<T*>(p.dgate) + at, (v * TPR + t) * 8, p.width, active, dz);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float n = (x[e] - mean) * rstd;
+                if (active) {
+                    dw[v][e] = fmaf(dh[v][e], n, dw[v][e]);
+                    db[v][e] += dh[v][e];
+                }
+                dh[v][e] *= w[v][e];
+                c0 += dh[v][e];
+                c1 = fmaf(dh[v][e], n, c1);
+            }
+        }
+        row_sums<TPR>(c0, c1, box, turn);
+        c0 = p.rms ? 0.f : c0 * p.inv_width;
+        c1 *= p.inv_width;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float x[8];
+            raw[v].get(x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = rstd * (dh[v][e] - c0 - (x[e] - mean) * rstd * c1);
+            store8<T, VEC>(static_cast<T*>(p.dx) + at, (v * TPR + t) * 8, p.width, active, x);
+        }
+    }
+    launch_dependents();
+    if (p.partial == nullptr) return;
+    float* const mine = p.partial + static_cast<long long>(blockIdx.x) * 2 * p.width;
+#pragma unroll 1
+    for (int which = 0; which < (p.want_db ? 2 : 1); ++which) {
+        if (G == 1) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int col = (v * TPR + t) * 8 + e;
+                    if (col < p.width) mine[which * p.width + col] = which ? db[v][e] : dw[v][e];
+                }
+            continue;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) gather[(threadIdx.x / TPR) * kColumns + (v * TPR + t) * 8 + e] = which ? db[v][e] : dw[v][e];
+        __syncthreads();
+        for (int col = threadIdx.x; col < p.width; col += cta_threads<TPR>()) {
+            float s = 0.f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) s += gather[g * kColumns + col];
+            mine[which * p.width + col] = s;
+        }
+    }
+}
+
+// The CTAs' sums of dw and db, added in order of the CTAs (32 columns a CTA, 32 rows of them at a time)
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, int parts, int width, float* dw, float* db) {
+    __shared__ float box[32][33];
+    grid_dependency_wait();
+    const int col = blockIdx.x * 32 + threadIdx.x;
+    float* const out = blockIdx.y ? db : dw;
+    if (out == nullptr) return;
+    float s = 0.f;
+    if (col < width)
+#pragma unroll 4
+        for (int i = threadIdx.y; i < parts; i += 32) s += partial[(static_cast<long long>(i) * 2 + blockIdx.y) * width + col];
+    box[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.y == 0 && col < width) {
+        s = 0.f;
+        for (int i = 0; i < 32; ++i) s += box[i][threadIdx.x];
+        out[col] = s;
+    }
+}
+
+constexpr int kForwardPerSM = 8, kBackwardPerSM = 4;  // CTAs of 256 threads that a launch brings, at most
+
+// threads of a row, and rows that a CTA has at a time
+int row_threads(int width) { return width <= 128 ? 16 : width <= 1024 ? 32 : width <= 8192 ? 256 : 512; }
+long long cta_count(long long rows, int width, int per_sm) {
+    const int tpr = row_threads(width);
+    const int g = tpr > kNormThreads ? 1 : kNormThreads / tpr;
+    const long long need = (rows + g - 1) / g, most = static_cast<long long>(per_sm) * kSMs;
+    return need < most ? need : most;
+}
+
+template <typename T, int NV, int TPR>
+int launch_norm(const ParamsN& p, bool backward, cudaStream_t stream) {
+    const bool vec = p.width % 8 == 0;
+    const unsigned grid = static_cast<unsigned>(cta_count(p.rows, p.width, backward ? kBackwardPerSM : kForwardPerSM));
+    if (grid > 0) {
+        auto* kern = backward ? (vec ? norm_backward_kernel<T, NV, TPR, true> : norm_backward_kernel<T, NV, TPR, false>)
+                              : (vec ? norm_forward_kernel<T, NV, TPR, true> : norm_forward_kernel<T, NV, TPR, false>);
+        kern<<<grid, cta_threads<TPR>(), 0, stream>>>(p);
+        if (cudaGetLastError() != cudaSuccess) return GDN_ERR_LAUNCH;
+        count_launch();
+    }
+    return GDN_OK;
+}
+
+template <typename T>
+int launch_norm_width(const ParamsN& p, bool backward, cudaStream_t stream) {
+    const int w = p.width;
+    if (w <= 128) return launch_norm<T, 1, 16>(p, backward, stream);
+    if (w <= 256) return launch_norm<T, 1, 32>(p, backward, stream);
+    if (w <= 512) return launch_norm<T, 2, 32>(p, backward, stream);
+    if (w <= 1024) return launch_norm<T, 4, 32>(p, backward, stream);
+    if (w <= 2048) return launch_norm<T, 1, 256>(p, backward, stream);
+    if (w <= 4096) return launch_norm<T, 2, 256>(p, backward, stream);
+    if (w <= 8192) return launch_norm<T, 4, 256>(p, backward, stream);
+    return launch_norm<T, 4, 512>(p, backward, stream);
+}
+
+}  // namespace
+
+size_t norm_workspace(long long rows, int width) {
+    return static_cast<size_t>(cta_count(rows, width, kBackwardPerSM)) * 2 * width * sizeof(float);
+}
+
+int launch_layer_norm(const ProblemN& q, bool backward, cudaStream_t stream) {
+    ParamsN p{};
+    p.dy = q.dy, p.x = q.x, p.weight = q.weight, p.bias = q.bias, p.gate = q.gate;
+    p.y = q.y, p.dx = q.dx, p.dgate = q.dgate;
+    p.rows = q.rows, p.width = q.width, p.eps = q.eps, p.inv_width = 1.f / static_cast<float>(q.width);
+    p.rms = (q.flags & GDN_NORM_RMS) != 0, p.param_bf16 = q.param_dtype == GDN_DTYPE_BF16;
+    p.want_db = q.dbias != nullptr;
+    p.partial = backward && (q.dweight != nullptr || q.dbias != nullptr) ? static_cast<float*>(q.workspace) : nullptr;
+    const int rc = q.dtype == GDN_DTYPE_BF16 ? launch_norm_width<__nv_bfloat16>(p, backward, stream) : launch_norm_width<float>(p, backward, stream);
+    if (rc != GDN_OK || p.partial == nullptr) return rc;
+    const int parts = static_cast<int>(cta_count(q.rows, q.width, kBackwardPerSM));
+    float *const dw = q.dweight, *const db = q.dbias;
+    const dim3 grid((q.width + 31) / 32, db != nullptr ? 2 : 1);  // (without a weight there may be a bias)
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(32, 32);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, norm_sum_kernel, static_cast<const float*>(p.partial), parts, q.width, dw, db) != cudaSuccess) {
+        cudaGetLastError();
+        return GDN_ERR_LAUNCH;
+    }
+    count_launch();
+    return GDN_OK;
+}
+
+}  // namespace gdn
