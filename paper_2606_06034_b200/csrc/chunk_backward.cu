@@ -33,18 +33,20 @@ namespace {
 using namespace sm100;
 
 constexpr int kC = 64, kD = 128;
-constexpr int kSlice = 32;               // value features of a chain's CTA
-constexpr int kSlices = kD / kSlice;
 constexpr int kThreads = 256;
 
-// workspace of one chunk of one value head, in floats
-constexpr int kWsT = 0, kWsP = kWsT + kC * kC, kWsS = kWsP + kC * kC, kWsDS = kWsS + kD * kD, kWsU = kWsDS + kD * kD;
-constexpr int kWsZ = kWsU + kC * kD;     // z, then r in its place
+// workspace of one chunk of one value head, in floats. T and P: bf16 tiles of three pieces each (see split3); the states: tiles [v][64 keys] of
+// the upper two pieces; all as the products want them in shared memory. u, z, r [v][token]: a feature of the value per row, as the
+// chains have them in tensor memory.
+constexpr int kPieces = 3;
+constexpr int kWsT = 0, kWsP = kWsT + kPieces * kC * kC / 2, kWsS = kWsP + kPieces * kC * kC / 2, kWsDS = kWsS + kD * kD, kWsU = kWsDS + kD * kD;
+constexpr int kWsZ = kWsU + kC * kD;     // exp(g) z, then r in its place
 constexpr int kWsTab = kWsZ + kC * kD;   // tables of 64 floats each
 enum { TAB_EGK = 0, TAB_BETA, TAB_ECK, TAB_BEGK, TAB_SEGQ, TAB_G, TAB_RK, TAB_RQ, kTabs };
-constexpr int kWsDots = kWsTab + kTabs * kC;  // per slice: <r, v - exp(g) z>, beta exp(g) <r, z>, exp(g_C - g) <u, y>
-constexpr int kDots = 3;
-constexpr int kWsChunk = kWsDots + kSlices * kDots * kC;
+constexpr int kWsDots = kWsTab + kTabs * kC;  // exp(g) <r, z>, exp(g_C - g) <u, y>
+constexpr int kDots = 2;
+constexpr int kWsChunk = kWsDots + kDots * kC;
+static_assert(kWsChunk % 4 == 0, "16-byte pieces");
 
 struct Strides {  // of a token tensor, in elements
     long long seq, token, head;
@@ -57,6 +59,7 @@ struct ParamsB {
     __nv_bfloat16 *dQ, *dK, *dV;
     float *dbeta, *dg, *dS_in;
     float* ws;
+    int* status;
     const int* cu;  // packed sequences: their boundaries; null: n_seq sequences of T tokens
     int n_seq, T, H_k, H_v, group, chunks;  // chunks: of a dense sequence
     Strides qk, v, gate;
@@ -116,121 +119,54 @@ __device__ __forceinline__ void copy_rows(__nv_bfloat16* dst, const __nv_bfloat1
         cp16(dst + r * LD + c, r < rows ? src + r * row_stride + c : src, r < rows);
     }
 }
-// ROWS rows of COLS floats
-template <int LD, int ROWS, int COLS>
-__device__ __forceinline__ void copy_floats(float* dst, const float* src, int src_ld) {
-    for (int i = threadIdx.x; i < ROWS * (COLS / 4); i += kThreads) {
-        const int r = i / (COLS / 4), c = i % (COLS / 4) * 4;
-        cp16(dst + r * LD + c, src + r * src_ld + c, true);
-    }
-}
-
-// ---------------------------------------------------------------- tensor-core products
-// m16n8k8 tf32 and m16n8k16 bf16, fp32 accumulators. The sum index that lane c = lane % 4 holds in its two (four) places is 2c, 2c + 1
-// in both operands, which the sum does not notice: neighbours in memory, fetched together. Two tiles of columns are taken as a pair
-// that covers 16 columns in turn (even ones, odd ones): B of both is one fetch where the columns are neighbours in memory, and a thread's results are
-// four columns in a row: 4c, 4c + 2 in the first tile, 4c + 1, 4c + 3 in the second.
-// Row lengths in shared memory (in 32-bit words): 8 mod 32 for operands whose sum index runs along the row, 4 mod 16 for those where it
-// runs down the rows: no bank conflicts.
-__device__ __forceinline__ void mma_tf32(float (&d)[4], const float (&a)[4], float b0, float b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(__float_as_uint(a[0])), "r"(__float_as_uint(a[1])), "r"(__float_as_uint(a[2])), "r"(__float_as_uint(a[3])),
-                   "r"(__float_as_uint(b0)), "r"(__float_as_uint(b1)));
-}
+// ---------------------------------------------------------------- products in registers (the Gram matrices)
+// m16n8k16 bf16, fp32 accumulators
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// upper 11 bits of the mantissa (what tf32 holds); the rest
-__device__ __forceinline__ float tf_hi(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFFE000u); }
-template <int N>
-__device__ __forceinline__ void split(const float (&x)[N], float (&hi)[N], float (&lo)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) hi[i] = tf_hi(x[i]), lo[i] = x[i] - hi[i];
-}
 struct Lane {
-    int g, c;  // row of a fragment, place along the sum
+    int g, c;  // row of a fragment, pair of columns
     __device__ __forceinline__ Lane() : g((threadIdx.x % 32) / 4), c(threadIdx.x % 4) {}
 };
-// A[m][k] = x[m * ld + k]
-__device__ __forceinline__ void a_rows(const float* x, int ld, int m0, int k0, const Lane& l, float (&a)[4]) {
-    const float2 u = *reinterpret_cast<const float2*>(x + (m0 + l.g) * ld + k0 + 2 * l.c);
-    const float2 v = *reinterpret_cast<const float2*>(x + (m0 + l.g + 8) * ld + k0 + 2 * l.c);
-    a[0] = u.x, a[2] = u.y, a[1] = v.x, a[3] = v.y;
-}
-__device__ __forceinline__ void a_rows(const __nv_bfloat16* x, int ld, int m0, int k0, const Lane& l, float (&a)[4]) {
-    const uint32_t u = *reinterpret_cast<const uint32_t*>(x + (m0 + l.g) * ld + k0 + 2 * l.c);
-    const uint32_t v = *reinterpret_cast<const uint32_t*>(x + (m0 + l.g + 8) * ld + k0 + 2 * l.c);
-    a[0] = bf16_lo(u), a[2] = bf16_hi(u), a[1] = bf16_lo(v), a[3] = bf16_hi(v);
-}
-// A[m][k] = x[k * ld + m]
-__device__ __forceinline__ void a_cols(const float* x, int ld, int m0, int k0, const Lane& l, float (&a)[4]) {
-    const float* const q = x + (k0 + 2 * l.c) * ld + m0 + l.g;
-    a[0] = q[0], a[1] = q[8], a[2] = q[ld], a[3] = q[ld + 8];
-}
-// a pair of tiles, B[k][n] = x[k * ld + n]: b[0], b[1] of the first tile, b[2], b[3] of the second
-__device__ __forceinline__ void b_cols(const float* x, int ld, int n0, int k0, const Lane& l, float (&b)[4]) {
-    const float2 u = *reinterpret_cast<const float2*>(x + (k0 + 2 * l.c) * ld + n0 + 2 * l.g);
-    const float2 v = *reinterpret_cast<const float2*>(x + (k0 + 2 * l.c + 1) * ld + n0 + 2 * l.g);
-    b[0] = u.x, b[2] = u.y, b[1] = v.x, b[3] = v.y;
-}
-__device__ __forceinline__ void b_cols(const __nv_bfloat16* x, int ld, int n0, int k0, const Lane& l, float (&b)[4]) {
-    const uint32_t u = *reinterpret_cast<const uint32_t*>(x + (k0 + 2 * l.c) * ld + n0 + 2 * l.g);
-    const uint32_t v = *reinterpret_cast<const uint32_t*>(x + (k0 + 2 * l.c + 1) * ld + n0 + 2 * l.g);
-    b[0] = bf16_lo(u), b[2] = bf16_hi(u), b[1] = bf16_lo(v), b[3] = bf16_hi(v);
-}
-// a pair of tiles, B[k][n] = x[n * ld + k]
-__device__ __forceinline__ void b_rows(const float* x, int ld, int n0, int k0, const Lane& l, float (&b)[4]) {
-    const float2 u = *reinterpret_cast<const float2*>(x + (n0 + 2 * l.g) * ld + k0 + 2 * l.c);
-    const float2 v = *reinterpret_cast<const float2*>(x + (n0 + 2 * l.g + 1) * ld + k0 + 2 * l.c);
-    b[0] = u.x, b[1] = u.y, b[2] = v.x, b[3] = v.y;
-}
-// one pair of tiles += A B, with A, B exact in tf32 / one of them split / both split
-__device__ __forceinline__ void pair_1(float (&d)[2][4], const float (&a)[4], const float (&b)[4]) {
-    mma_tf32(d[0], a, b[0], b[1]);
-    mma_tf32(d[1], a, b[2], b[3]);
-}
-__device__ __forceinline__ void pair_b2(float (&d)[2][4], const float (&a)[4], const float (&b)[4]) {
-    float hi[4], lo[4];
-    split(b, hi, lo);
-    pair_1(d, a, lo);
-    pair_1(d, a, hi);
-}
-__device__ __forceinline__ void pair_a2(float (&d)[2][4], const float (&a)[4], const float (&b)[4]) {
-    float hi[4], lo[4];
-    split(a, hi, lo);
-    pair_1(d, lo, b);
-    pair_1(d, hi, b);
-}
-__device__ __forceinline__ void pair_3(float (&d)[2][4], const float (&a)[4], const float (&b)[4]) {
-    float ah[4], al[4], bh[4], bl[4];
-    split(a, ah, al);
-    split(b, bh, bl);
-    pair_1(d, al, bh);
-    pair_1(d, ah, bl);
-    pair_1(d, ah, bh);
-}
-// the four neighbouring results of a thread in row g (half = 0) or g + 8 (half = 1) of a pair
-__device__ __forceinline__ float4 pair_row(const float (&d)[2][4], int half) {
-    return make_float4(d[0][2 * half], d[1][2 * half], d[0][2 * half + 1], d[1][2 * half + 1]);
-}
-__device__ __forceinline__ float dot4(float4 a, float4 b) { return a.x * b.x + a.y * b.y + a.z * b.z + a.w * b.w; }
-__device__ __forceinline__ float4 scaled(float4 a, float s) { return make_float4(a.x * s, a.y * s, a.z * s, a.w * s); }
-__device__ __forceinline__ float4 bf16x4(uint2 w) { return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)); }
 __device__ __forceinline__ float quad_sum(float x) {
     x += __shfl_xor_sync(0xffffffffu, x, 1);
     return x + __shfl_xor_sync(0xffffffffu, x, 2);
 }
 
-constexpr int kLdX = 136;  // bf16 rows of 128 features: 68 words
-constexpr int kLdF = 136;  // fp32 rows of 128, sum index along the row
-constexpr int kLdN = 132;  // fp32 rows of 128, sum index down the rows (or pairs of rows)
-constexpr int kLdM = 72;   // fp32 rows of 64, sum index along the row
-constexpr int kLdV = 68;   // fp32 rows of 64, sum index down the rows
-constexpr int kLdS = 36;   // fp32 rows of a slice's 32 features, sum index down the rows
-constexpr int kLdO = 40;   // bf16 rows of a slice's 32 features: 20 words
+constexpr int kLdX = 136;  // bf16 rows of 128 features: 68 words, no bank conflicts
+constexpr int kLdV = 68;   // fp32 rows of 64
+
+// A value as three bf16 pieces, x = h - m + l (the middle one negated: that is how the difference comes out of one instruction): 24 bits
+__device__ __forceinline__ float bf16_minus_lo(uint32_t w, float x) {
+    float r;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tsub.f32.bf16 %0, a, %2;\n\t}" : "=f"(r) : "r"(w), "f"(x));
+    return r;
+}
+__device__ __forceinline__ float bf16_minus_hi(uint32_t w, float x) {
+    float r;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %1;\n\tsub.f32.bf16 %0, b, %2;\n\t}" : "=f"(r) : "r"(w), "f"(x));
+    return r;
+}
+__device__ __forceinline__ void split3(float x, float y, uint32_t& h, uint32_t& m, uint32_t& l) {
+    h = pack_bf16x2(x, y);
+    const float a = bf16_minus_lo(h, x), b = bf16_minus_hi(h, y);
+    m = pack_bf16x2(a, b);
+    l = pack_bf16x2(bf16_minus_lo(m, a), bf16_minus_hi(m, b));
+}
+// Byte of element (row, col) of a 64 x 64 bf16 tile in the 128-byte swizzle: 16-byte pieces of a row change places with its number mod 8
+__device__ __forceinline__ int swizzled(int row, int col) { return row * 128 + ((((col >> 3) ^ row) & 7) << 4) + (col & 7) * 2; }
+constexpr int kTile = kC * kC * 2;  // bytes of such a tile
+// four neighbours of a row into the three tiles of a matrix
+__device__ __forceinline__ void store_pieces(float* tiles, int row, int col, const float (&x)[4]) {
+    uint32_t w[kPieces][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) split3(x[2 * e], x[2 * e + 1], w[0][e], w[1][e], w[2][e]);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(tiles) + i * kTile + swizzled(row, col)) = make_uint2(w[i][0], w[i][1]);
+}
 
 // ---------------------------------------------------------------- T, P and the gates' tables
 struct SmemSystem {
@@ -339,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) chunk_system_kernel(const ParamsB p)
                 q[e] = j <= row ? gam * sm.qk[row * kLdV + j] : 0.f;
             }
             *reinterpret_cast<float4*>(sm.A + row * kLdV + col) = make_float4(a[0], a[1], a[2], a[3]);
-            *reinterpret_cast<float4*>(ws + kWsP + row * kC + col) = make_float4(q[0], q[1], q[2], q[3]);
+            store_pieces(ws + kWsP, row, col, q);
         }
         __syncthreads();
         {  // column j of T by forward substitution: x_i = [i = j] - sum_k A_ik x_k, four threads a column
@@ -364,592 +300,1114 @@ __global__ void __launch_bounds__(kThreads) chunk_system_kernel(const ParamsB p)
         __syncthreads();
         for (int i = tid; i < kC * kC / 4; i += kThreads) {
             const int row = i / 16, col = i % 16 * 4;
-            *reinterpret_cast<float4*>(ws + kWsT + row * kC + col) = *reinterpret_cast<const float4*>(sm.T + row * kLdV + col);
+            const float4 x = *reinterpret_cast<const float4*>(sm.T + row * kLdV + col);
+            const float t[4] = {x.x, x.y, x.z, x.w};
+            store_pieces(ws + kWsT, row, col, t);
         }
     }
 }
 
-// ---------------------------------------------------------------- the states, forward over the chunks
+// ---------------------------------------------------------------- the chains over the chunks: tcgen05, the value's features on the lanes
+// One CTA has a (sequence, value head). Everything is kept transposed, a feature of the value on each of the 128 lanes of tensor memory: S
+// and D [v x key], and z, u, y, r [v x token]. The fp32 operand of a product, split into three bf16 pieces, is A, in tensor memory; B is a tile in
+// shared memory: K or Q as they are (both ways round), T or P in pieces. All sums are fp32 in tensor memory; the state itself stays in registers
+// (64 values a thread) and takes the chunk's part, summed on its own, with one fma.
+// Eight warps: two for each quarter of the lanes, each with half of the columns. Registers have the layout of the 16 x 256 bit loads:
+// row (lane / 4) and row + 8 of 16 lanes, columns 2 (lane mod 4) and the next of every 8. In it a warp's 8-byte stores fill whole sectors.
+constexpr int kLdT = 136;  // rows of the tiles that ldmatrix turns, in bf16: 272 bytes, no bank conflicts
+constexpr uint32_t kNegA = 1u << 13;  // instruction descriptor: A negated
+
+__device__ __forceinline__ void tm_ld64(uint32_t taddr, float (&x)[32]) {  // 16 lanes x 64 columns
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tm_ld32(uint32_t taddr, float (&x)[16]) {  // 16 lanes x 32 columns
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
+}
+// the reverse for packed pairs: 16 lanes x 16 or 32 columns of pairs
+__device__ __forceinline__ void tm_st_pairs(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+__device__ __forceinline__ void tm_st_pairs(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// 2 N values of 16 lanes, split, into the columns of the three pieces (`apart` columns from one piece to the next)
+template <int N>
+__device__ __forceinline__ void tm_st_split(uint32_t taddr, uint32_t apart, const float (&x)[2 * N]) {
+    uint32_t h[N], m[N], l[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) split3(x[2 * i], x[2 * i + 1], h[i], m[i], l[i]);
+    tm_st_pairs(taddr, h);
+    tm_st_pairs(taddr + apart, m);
+    tm_st_pairs(taddr + 2 * apart, l);
+}
+// [token][feature] rows turned: four 8 x 8 blocks, tokens t0 .. t0 + 15 and features v0 .. v0 + 15, as pairs of tokens: w[0], w[1] features
+// v0 .. and v0 + 8 .. of the first 8 tokens, w[2], w[3] of the others (the layout of the accumulators' registers)
+__device__ __forceinline__ void turned(const __nv_bfloat16* tile, int t0, int v0, uint32_t (&w)[4]) {
+    const int lane = threadIdx.x % 32;
+    const uint32_t at = smem_u32(tile + (t0 + (lane & 7) + (lane >> 4) * 8) * kLdT + v0 + ((lane >> 3) & 1) * 8);
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+}
+// 64 rows of 128 bf16 by N threads: as two tiles of 64 x 64 in the 128-byte swizzle, `apart` bytes from one to the other / as rows of kLdT;
+// rows from `rows` on are zeros
+template <int N>
+__device__ __forceinline__ void copy_tile(uint8_t* dst, const __nv_bfloat16* src, long long row_stride, int rows, int me, int apart = kTile) {
+    static_assert(N % 16 == 0, "");
+    const int c = me % 16 * 8;
+    src += me / 16 * row_stride + c;
+    dst += c / 64 * apart;
+#pragma unroll 8
+    for (int r = me / 16; r < kC; r += N / 16) {
+        cp16(dst + swizzled(r, c % 64), r < rows ? src : src - (r - me / 16) * row_stride - me / 16 * row_stride, r < rows);
+        src += N / 16 * row_stride;
+    }
+}
+template <int N>
+__device__ __forceinline__ void copy_plain(__nv_bfloat16* dst, const __nv_bfloat16* src, long long row_stride, int rows, int me) {
+    const int c = me % 16 * 8;
+    src += me / 16 * row_stride + c;
+#pragma unroll 8
+    for (int r = me / 16; r < kC; r += N / 16) {
+        cp16(dst + r * kLdT + c, r < rows ? src : src - (r - me / 16) * row_stride - me / 16 * row_stride, r < rows);
+        src += N / 16 * row_stride;
+    }
+}
+// whole runs of bytes (multiples of 16): one thread asks, the copy engine does it
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)), "r"(smem_u32(src)), "r"(bytes) : "memory");
+}
+
+// Bounded wait (about a second) of every thread for products in flight
+__device__ __forceinline__ bool wait_products(uint64_t* bar, uint32_t parity) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    uint32_t i = 0;
+    while (!mbar_try_wait_hint(bar, parity, 2000u))
+        if ((++i & 63u) == 0 && clock64() - t0 > 2000000000LL) return false;
+    return true;
+}
+// what a thread has written to tensor memory is there for whoever issues products behind the next barrier
+__device__ __forceinline__ void publish() {
+    tmem_wait_st();
+    tc_fence_before_sync();
+}
+// hand-offs: `from` threads arrive and go on, a warp waits. Each is passed once a chunk, and a barrier of the whole CTA lies between two chunks.
+template <int ID>
+__device__ __forceinline__ void arrive() {
+    asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kThreads + 32) : "memory");
+}
+template <int ID>
+__device__ __forceinline__ void await() {
+    asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kThreads + 32) : "memory");
+}
+
+// Products of the chains, each issued by one thread. A [128 lanes x K] in three pieces of K / 2 columns at `a`; the small ones first.
+__device__ __forceinline__ uint64_t desc_rows(uint32_t tile) { return smem_desc(tile, 16, 1024, SWZ_128B); }      // sum index along the rows
+__device__ __forceinline__ uint64_t desc_cols(uint32_t tile) { return smem_desc(tile, kTile, 1024, SWZ_128B); }  // sum index down the rows
+constexpr uint32_t kIdescRows = instr_desc(128, 64, 1, 1, 0, 0, 1), kIdescCols = instr_desc(128, 64, 1, 1, 0, 1, 1);
+// d = A X^T, X: 64 rows of 128 bf16 (two tiles)
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t x) {
+    const uint64_t b = desc_rows(x);
+#pragma unroll
+    for (int i = kPieces - 1; i >= 0; --i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            mma_f16_ts(d, a + i * 64 + k * 8, b + ((k >> 2) * kTile + (k & 3) * 32) / 16, kIdescRows | (i == 1 ? kNegA : 0u), i < kPieces - 1 || k > 0);
+}
+// d (128 columns, += if `more`) = A X, A [128 x 64 tokens], X as above
+__device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t x, bool more) {
+    const uint64_t b = desc_cols(x);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = kPieces - 1; i >= 0; --i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                mma_f16_ts(d + half * 64, a + i * 32 + k * 8, b + (half * kTile + k * 2048) / 16, kIdescCols | (i == 1 ? kNegA : 0u),
+                           more || i < kPieces - 1 || k > 0);
+}
+// d = A M^T (COLS: A M), both in three pieces, M 64 x 64 in three tiles: the six products of pieces that fp32 can hold
+template <bool COLS>
+__device__ __forceinline__ void product_system(uint32_t d, uint32_t a, uint32_t tiles) {
+    const uint64_t b = COLS ? desc_cols(tiles) : desc_rows(tiles);
+    bool more = false;
+#pragma unroll
+    for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+        for (int i = sum; i >= 0; --i) {
+            const int j = sum - i;  // the pieces of A and M; one middle piece: negated
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                mma_f16_ts(d, a + i * 32 + k * 8, b + (j * kTile + k * (COLS ? 2048 : 32)) / 16,
+                           (COLS ? kIdescCols : kIdescRows) | ((i == 1) != (j == 1) ? kNegA : 0u), more);
+                more = true;
+            }
+        }
+}
+
+// a value for each of a thread's 8 x 2 rows and columns: `f(row, column, i)` gets the place of x[i], x[i + 1] (neighbouring columns)
+template <int N, typename F>
+__device__ __forceinline__ void for_pairs(const F& f) {
+    const Lane l;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) f(l.g + ((i >> 1) & 1) * 8, (i >> 2) * 8 + 2 * l.c, i);
+}
+
+constexpr int kChainThreads = kThreads + 64;  // eight warps that compute, one that issues the products, one that loads and stores tiles
+constexpr int kImage = 2 * 2 * 2 * kTile;     // bytes of a state's tiles: two pieces of two tiles of 128 rows
+// Byte of element (row, col) of a state in its image
+__device__ __forceinline__ int image_at(int piece, int row, int col) { return (piece * 2 + col / 64) * 2 * kTile + swizzled(row, col % 64); }
+// this thread's part of a state (see for_pairs) into the image
+__device__ __forceinline__ void put_image(uint8_t* image, const float (&S)[2][32], int row0, int half) {
+#pragma unroll
+    for (int lh = 0; lh < 2; ++lh)
+        for_pairs<32>([&](int row, int col, int i) {
+            const uint32_t h = pack_bf16x2(S[lh][i], S[lh][i + 1]);
+            const uint32_t m = pack_bf16x2(bf16_minus_lo(h, S[lh][i]), bf16_minus_hi(h, S[lh][i + 1]));
+            uint8_t* const at = image + image_at(0, row0 + lh * 16 + row, half * 64 + col);
+            *reinterpret_cast<uint32_t*>(at) = h;
+            *reinterpret_cast<uint32_t*>(at + kImage / 2) = m;
+        });
+}
+
+// tensor memory: the state's part of the chunk (128 columns), the state's pieces, z or u, the pieces of the right-hand side or of u
+constexpr uint32_t kTmDelta = 0, kTmState = 128, kTmAcc = 320, kTmRhs = 384, kTmColumns = 512;
+
+struct Chain {
+    uint64_t *done, *full;  // products complete; copies of a chunk's tiles complete
+    uint32_t tm, lanes;     // base; this warp's lanes in the address
+    uint32_t phase = 0;
+    bool failed = false;
+    __device__ __forceinline__ void wait() {
+        failed |= !wait_products(done, phase);
+        phase ^= 1;
+        tc_fence_after_sync();
+    }
+};
+__device__ __forceinline__ void chain_begin(Chain& ch, uint64_t* bars, uint32_t* base, uint32_t columns) {
+    if (threadIdx.x == 0) {
+        mbar_init(bars, 1);
+        mbar_init(bars + 1, 1);
+        mbar_fence_init();
+    }
+    if (threadIdx.x < 32) {
+        tmem_alloc(base, columns);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    ch.done = bars;
+    ch.full = bars + 1;
+    ch.tm = *base;
+    ch.lanes = static_cast<uint32_t>(threadIdx.x / 32 % 4 * 32) << 16;
+}
+__device__ __forceinline__ void chain_end(Chain& ch, int* status, uint32_t columns) {
+    if (ch.failed) *status = GDN_ERR_TIMEOUT;
+    tc_fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x < 32) tmem_dealloc(ch.tm, columns);
+}
+
+// Forward: z, u and the state at the start of every chunk. A chunk's chain is three products (24 of 128 x 64 x 16 each) and, between them, the
+// splitting of what the next one reads: z -> right-hand side -> u -> state. What goes to memory (the state, z, u) goes while products run.
 struct StageF {
-    __nv_bfloat16 K[kC * kLdX];
-    float T[kC * kLdM];
+    uint8_t K[2 * kTile], T[kPieces * kTile];
     float tab[kTabs * kC];
+    __nv_bfloat16 V[kC * kLdT];
+    uint8_t pad[1024 - (kC * kLdT * 2 + kTabs * kC * 4) % 1024];  // the tiles lie on 1 KB
 };
 struct SmemF {
     StageF stage[2];
-    float S[kSlice * kLdN];
-    float R[kC * kLdS], U[kC * kLdS];
+    uint8_t image[kImage];
 };
 
-__global__ void __launch_bounds__(kThreads) chunk_states_kernel(const ParamsB p) {
+__global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const ParamsB p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    SmemF& sm = *reinterpret_cast<SmemF*>(smem_raw);
-    const int slice = blockIdx.x % kSlices, h = blockIdx.x / kSlices % p.H_v, s = blockIdx.x / kSlices / p.H_v;
+    SmemF& sm = *reinterpret_cast<SmemF*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
+    __shared__ uint64_t bars[2];
+    __shared__ uint32_t base;
+    const int h = blockIdx.x % p.H_v, s = blockIdx.x / p.H_v, hk = h / p.group;
     const Seq seq = seq_of(p, s);
     const int n = (seq.len + kC - 1) / kC;
-    const int tid = threadIdx.x, warp = tid / 32;
-    const Lane l;
-    const int hk = h / p.group;
-    const auto load = [&](int c) {
-        if (c < n) {
+    const int warp = threadIdx.x / 32;
+    Chain ch;
+    chain_begin(ch, bars, &base, kTmColumns);
+    if (warp == kThreads / 32) {  // ---- the products
+        for (int c = 0; c < n; ++c) {
             StageF& st = sm.stage[c % 2];
-            const float* const ws = chunk_ws(p, seq.slot + c, h);
-            copy_rows<kLdX, kD>(st.K, p.K + p.qk.at(s, seq.first + c * kC, hk), p.qk.token, seq.len - c * kC);
-            copy_floats<kLdM, kC, kC>(st.T, ws + kWsT, kC);
-            copy_floats<kTabs * kC, 1, kTabs * kC>(st.tab, ws + kWsTab, 0);
-        }
-        cp_commit();
-    };
-    load(0);
-    // tokens x features: 16 x 16 a warp
-    const int m0 = warp % 4 * 16, n0 = warp / 4 * 16;
-    const int v0 = slice * kSlice + n0 + 4 * l.c;  // this thread's four features
-    // the state: 32 features x 16 keys a warp, in registers (fragments) and, for the first product, in shared memory
-    float S[2][2][4];
-    const float* const S_in = p.S_in == nullptr ? nullptr : p.S_in + ((static_cast<long long>(s) * p.H_v + h) * kD + slice * kSlice) * kD;
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int row = mt * 16 + half * 8 + l.g, col = warp * 16 + 4 * l.c;
-            const float4 x = S_in == nullptr ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(S_in + row * kD + col);
-            S[mt][0][2 * half] = x.x, S[mt][1][2 * half] = x.y, S[mt][0][2 * half + 1] = x.z, S[mt][1][2 * half + 1] = x.w;
-            *reinterpret_cast<float4*>(sm.S + row * kLdN + col) = x;
-        }
-    for (int c = 0; c < n; ++c) {
-        const StageF& st = sm.stage[c % 2];
-        float* const ws = chunk_ws(p, seq.slot + c, h);
-        const int t0 = c * kC;
-        float4 v[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int t = t0 + m0 + half * 8 + l.g;
-            v[half] = t < seq.len ? bf16x4(*reinterpret_cast<const uint2*>(p.V + p.v.at(s, seq.first + t, h) + v0)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-                *reinterpret_cast<float4*>(ws + kWsS + (slice * kSlice + mt * 16 + half * 8 + l.g) * kD + warp * 16 + 4 * l.c) = pair_row(S[mt], half);
-        cp_wait<0>();
-        __syncthreads();  // the chunk's operands are there, the state's copy is written, the last chunk's stage is free
-        load(c + 1);
-        float z[2][4] = {};
-#pragma unroll
-        for (int k0 = 0; k0 < kD; k0 += 8) {
-            float a[4], b[4];
-            a_rows(st.K, kLdX, m0, k0, l, a);
-            b_rows(sm.S, kLdN, n0, k0, l, b);
-            pair_b2(z, a, b);
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = m0 + half * 8 + l.g;
-            const float e = st.tab[TAB_EGK * kC + i], beta = st.tab[TAB_BETA * kC + i];
-            const float4 x = scaled(pair_row(z, half), e);  // exp(g_i) S k_i
-            *reinterpret_cast<float4*>(ws + kWsZ + i * kD + v0) = x;
-            *reinterpret_cast<float4*>(sm.R + i * kLdS + n0 + 4 * l.c) =
-                make_float4(beta * (v[half].x - x.x), beta * (v[half].y - x.y), beta * (v[half].z - x.z), beta * (v[half].w - x.w));
-        }
-        __syncthreads();
-        float u[2][4] = {};
-        for (int k0 = 0; k0 < m0 + 16; k0 += 8) {  // T is lower triangular
-            float a[4], b[4];
-            a_rows(st.T, kLdM, m0, k0, l, a);
-            b_cols(sm.R, kLdS, n0, k0, l, b);
-            pair_3(u, a, b);
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = m0 + half * 8 + l.g;
-            const float4 x = pair_row(u, half);
-            *reinterpret_cast<float4*>(ws + kWsU + i * kD + v0) = x;
-            *reinterpret_cast<float4*>(sm.U + i * kLdS + n0 + 4 * l.c) = scaled(x, st.tab[TAB_ECK * kC + i]);
-        }
-        __syncthreads();
-        const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            float d[2][4] = {};
-#pragma unroll
-            for (int k0 = 0; k0 < kC; k0 += 8) {
-                float a[4], b[4];
-                a_cols(sm.U, kLdS, mt * 16, k0, l, a);
-                b_cols(st.K, kLdX, warp * 16, k0, l, b);
-                pair_a2(d, a, b);
+            const uint32_t tileK = smem_u32(st.K), tileT = smem_u32(st.T);
+            ch.failed |= !wait_products(ch.full, c & 1);  // (before the barrier: behind it the next copies are asked for)
+            if (__syncthreads_or(ch.failed)) break;
+            tc_fence_after_sync();
+            if (elect_one()) {
+                product_rows(ch.tm + kTmAcc, ch.tm + kTmState, tileK);
+                mma_commit(ch.done);
             }
+            __syncwarp();
+            await<1>();
+            tc_fence_after_sync();
+            if (elect_one()) {
+                product_system<false>(ch.tm + kTmAcc, ch.tm + kTmRhs, tileT);
+                mma_commit(ch.done);
+            }
+            __syncwarp();
+            await<2>();
+            tc_fence_after_sync();
+            if (elect_one()) {
+                product_cols(ch.tm + kTmDelta, ch.tm + kTmRhs, tileK, false);
+                mma_commit(ch.done);
+            }
+            __syncwarp();
+        }
+    } else if (warp > kThreads / 32) {  // ---- the tiles
+        const int me = threadIdx.x % 32;
+        const auto load = [&](int c) {
+            if (c < n) {
+                StageF& st = sm.stage[c % 2];
+                const float* const ws = chunk_ws(p, seq.slot + c, h);
+                if (me == 0) {
+                    mbar_arrive_expect_tx(ch.full, sizeof(st.T) + sizeof(st.tab));
+                    bulk_load(st.T, ws + kWsT, sizeof(st.T), ch.full);
+                    bulk_load(st.tab, ws + kWsTab, sizeof(st.tab), ch.full);
+                }
+                copy_tile<32>(st.K, p.K + p.qk.at(s, seq.first + c * kC, hk), p.qk.token, seq.len - c * kC, me);
+                copy_plain<32>(st.V, p.V + p.v.at(s, seq.first + c * kC, h), p.v.token, seq.len - c * kC, me);
+                cp_commit();
+            }
+        };
+        load(0);
+        for (int c = 0; c < n; ++c) {
+            cp_wait<0>();
+            tma_store_wait_read<0>();  // the image may be written again
+            fence_proxy_async_smem();
+            ch.failed |= !wait_products(ch.full, c & 1);
+            if (__syncthreads_or(ch.failed)) break;
+            load(c + 1);
+            await<3>();
+            if (me == 0) {
+                bulk_store(chunk_ws(p, seq.slot + c, h) + kWsS, sm.image, kImage);
+                tma_store_commit();
+            }
+            __syncwarp();
+        }
+        tma_store_wait_all<0>();
+    } else {  // ---- what lies between the products
+        const int half = warp / 4, row0 = warp % 4 * 32;
+        float S[2][32];
+        const long long state = (static_cast<long long>(s) * p.H_v + h) * kD * kD;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+        for (int lh = 0; lh < 2; ++lh)
+            for_pairs<32>([&](int row, int col, int i) {
+                const float2 x = p.S_in == nullptr ? make_float2(0.f, 0.f)
+                                                   : *reinterpret_cast<const float2*>(p.S_in + state + (row0 + lh * 16 + row) * kD + half * 64 + col);
+                S[lh][i] = x.x, S[lh][i + 1] = x.y;
+            });
+        for (int c = 0; c < n; ++c) {
+            const StageF& st = sm.stage[c % 2];
+            float* const ws = chunk_ws(p, seq.slot + c, h);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[mt][x][e] = fmaf(decay, S[mt][x][e], d[x][e]);
+            for (int lh = 0; lh < 2; ++lh) tm_st_split<16>(ch.tm + ch.lanes + (lh << 20) + kTmState + half * 32, 64, S[lh]);
+            publish();
+            if (__syncthreads_or(ch.failed)) break;
+            put_image(sm.image, S, row0, half);
+            fence_proxy_async_smem();
+            arrive<3>();
+            uint32_t v[2][8];
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-                *reinterpret_cast<float4*>(sm.S + (mt * 16 + half * 8 + l.g) * kLdN + warp * 16 + 4 * l.c) = pair_row(S[mt], half);
+            for (int lh = 0; lh < 2; ++lh)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) turned(st.V, half * 32 + q * 16, row0 + lh * 16, reinterpret_cast<uint32_t(&)[4]>(v[lh][q * 4]));
+            ch.wait();
+            float z[2][16];
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float x[16];
+                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, z[lh]);
+                tmem_wait_ld();
+                for_pairs<16>([&](int, int col, int i) {
+                    const int t = half * 32 + col;
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_EGK * kC + t), b = *reinterpret_cast<const float2*>(st.tab + TAB_BETA * kC + t);
+                    z[lh][i] *= e.x, z[lh][i + 1] *= e.y;
+                    x[i] = b.x * (bf16_lo(v[lh][i / 2]) - z[lh][i]), x[i + 1] = b.y * (bf16_hi(v[lh][i / 2]) - z[lh][i + 1]);
+                });
+                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmRhs + half * 16, 32, x);
+            }
+            publish();
+            arrive<1>();
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh)
+                for_pairs<16>([&](int row, int col, int i) {
+                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + half * 32 + col) = make_float2(z[lh][i], z[lh][i + 1]);
+                });
+            ch.wait();
+            float u[2][16];
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float x[16];
+                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, u[lh]);
+                tmem_wait_ld();
+                for_pairs<16>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_ECK * kC + half * 32 + col);
+                    x[i] = u[lh][i] * e.x, x[i + 1] = u[lh][i + 1] * e.y;
+                });
+                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmRhs + half * 16, 32, x);
+            }
+            publish();
+            arrive<2>();
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh)
+                for_pairs<16>([&](int row, int col, int i) {
+                    *reinterpret_cast<float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + half * 32 + col) = make_float2(u[lh][i], u[lh][i + 1]);
+                });
+            const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
+            ch.wait();
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float x[32];
+                tm_ld64(ch.tm + ch.lanes + (lh << 20) + kTmDelta + half * 64, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) S[lh][i] = fmaf(decay, S[lh][i], x[i]);
+            }
         }
     }
+    chain_end(ch, p.status, kTmColumns);
 }
 
-// ---------------------------------------------------------------- their gradients, backward over the chunks
+// Backward: r and the state's gradient at the end of every chunk.
 struct StageB {
-    __nv_bfloat16 K[kC * kLdX], Q[kC * kLdX], dO[kC * kLdO];
-    float T[kC * kLdV], P[kC * kLdV];
+    uint8_t K[2 * kTile], Q[2 * kTile];
     float tab[kTabs * kC];
+    __nv_bfloat16 dO[kC * kLdT];
+    uint8_t pad[1024 - (kC * kLdT * 2 + kTabs * kC * 4) % 1024];
 };
 struct SmemB {
     StageB stage[2];
-    float D[kSlice * kLdN];
-    float du[kC * kLdS], w[2 * kC * kLdS];  // w: scale exp(g) dO, then -beta exp(g) r
-    float dots[2][kDots][kC];
+    uint8_t T[kPieces * kTile], P[kPieces * kTile];  // (loaded again behind their last product of the chunk)
+    uint8_t image[kImage];
+    float dots[4][kDots][kC];
 };
+// tensor memory: the state's part; its gradient's pieces, and when these are used up those of du or -beta exp(g) r (96 columns) and of scale
+// exp(g) dO (96); y or r; P^T dO; dO
+constexpr uint32_t kTmDu = kTmState, kTmW = kTmState + 96, kTmX = 384, kTmO = 448;
 
-__global__ void __launch_bounds__(kThreads) chunk_state_grads_kernel(const ParamsB p) {
+__global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(const ParamsB p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    SmemB& sm = *reinterpret_cast<SmemB*>(smem_raw);
-    const int slice = blockIdx.x % kSlices, h = blockIdx.x / kSlices % p.H_v, s = blockIdx.x / kSlices / p.H_v;
+    SmemB& sm = *reinterpret_cast<SmemB*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
+    __shared__ uint64_t bars[2];
+    __shared__ uint32_t base;
+    const int h = blockIdx.x % p.H_v, s = blockIdx.x / p.H_v, hk = h / p.group;
     const Seq seq = seq_of(p, s);
     const int n = (seq.len + kC - 1) / kC;
-    const int tid = threadIdx.x, warp = tid / 32;
-    const Lane l;
-    const int hk = h / p.group;
-    const auto load = [&](int c) {
-        if (c >= 0) {
+    const int warp = threadIdx.x / 32;
+    Chain ch;
+    chain_begin(ch, bars, &base, kTmColumns);
+    if (warp == kThreads / 32) {  // ---- the products
+        uint32_t turn = 0;
+        for (int c = n - 1; c >= 0; --c) {
             StageB& st = sm.stage[c % 2];
-            const float* const ws = chunk_ws(p, seq.slot + c, h);
-            const int t = seq.first + c * kC, rows = seq.len - c * kC;
-            copy_rows<kLdX, kD>(st.K, p.K + p.qk.at(s, t, hk), p.qk.token, rows);
-            copy_rows<kLdX, kD>(st.Q, p.Q + p.qk.at(s, t, hk), p.qk.token, rows);
-            copy_rows<kLdO, kSlice>(st.dO, p.dO + p.v.at(s, t, h) + slice * kSlice, p.v.token, rows);
-            copy_floats<kLdV, kC, kC>(st.T, ws + kWsT, kC);
-            copy_floats<kLdV, kC, kC>(st.P, ws + kWsP, kC);
-            copy_floats<kTabs * kC, 1, kTabs * kC>(st.tab, ws + kWsTab, 0);
+            const uint32_t tileK = smem_u32(st.K), tileQ = smem_u32(st.Q);
+            ch.failed |= !wait_products(ch.full, turn);
+            turn ^= 1;
+            if (__syncthreads_or(ch.failed)) break;
+            tc_fence_after_sync();
+            if (elect_one()) product_rows(ch.tm + kTmAcc, ch.tm + kTmState, tileK);  // D K^T
+            __syncwarp();
+            await<1>();
+            tc_fence_after_sync();
+            if (elect_one()) {  // dO^T P
+                const uint64_t b = desc_cols(smem_u32(sm.P));
+#pragma unroll
+                for (int i = kPieces - 1; i >= 0; --i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        mma_f16_ts(ch.tm + kTmX, ch.tm + kTmO + k * 8, b + (i * kTile + k * 2048) / 16, kIdescCols | (i == 1 ? kNegA : 0u), i < kPieces - 1 || k > 0);
+                mma_commit(ch.done);
+            }
+            __syncwarp();
+            await<2>();
+            tc_fence_after_sync();
+            if (elect_one()) {
+                product_system<true>(ch.tm + kTmAcc, ch.tm + kTmDu, smem_u32(sm.T));
+                mma_commit(ch.done);
+            }
+            __syncwarp();
+            await<3>();
+            tc_fence_after_sync();
+            if (elect_one()) product_cols(ch.tm + kTmDelta, ch.tm + kTmW, tileQ, false);
+            __syncwarp();
+            await<4>();
+            tc_fence_after_sync();
+            if (elect_one()) {
+                product_cols(ch.tm + kTmDelta, ch.tm + kTmDu, tileK, true);
+                mma_commit(ch.done);
+            }
+            __syncwarp();
         }
-        cp_commit();
-    };
-    load(n - 1);
-    const int m0 = warp % 4 * 16, n0 = warp / 4 * 16;
-    const int v0 = slice * kSlice + n0 + 4 * l.c;
-    float D[2][2][4];
-    const long long state = ((static_cast<long long>(s) * p.H_v + h) * kD + slice * kSlice) * kD;
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int row = mt * 16 + half * 8 + l.g, col = warp * 16 + 4 * l.c;
-            const float4 x = p.dS_out == nullptr ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(p.dS_out + state + row * kD + col);
-            D[mt][0][2 * half] = x.x, D[mt][1][2 * half] = x.y, D[mt][0][2 * half + 1] = x.z, D[mt][1][2 * half + 1] = x.w;
-            *reinterpret_cast<float4*>(sm.D + row * kLdN + col) = x;
+    } else if (warp > kThreads / 32) {  // ---- the tiles
+        const int me = threadIdx.x % 32;
+        uint32_t turn = 0;
+        const auto load = [&](int c) {
+            if (c >= 0) {
+                StageB& st = sm.stage[c % 2];
+                const int t = seq.first + c * kC, rows = seq.len - c * kC;
+                copy_tile<32>(st.K, p.K + p.qk.at(s, t, hk), p.qk.token, rows, me);
+                copy_tile<32>(st.Q, p.Q + p.qk.at(s, t, hk), p.qk.token, rows, me);
+                copy_plain<32>(st.dO, p.dO + p.v.at(s, t, h), p.v.token, rows, me);
+                cp_commit();
+            }
+        };
+        const auto load_system = [&](int c) {
+            if (c >= 0 && me == 0) {
+                const float* const ws = chunk_ws(p, seq.slot + c, h);
+                mbar_arrive_expect_tx(ch.full, sizeof(sm.T) + sizeof(sm.P) + sizeof(sm.stage[0].tab));
+                bulk_load(sm.T, ws + kWsT, sizeof(sm.T) + sizeof(sm.P), ch.full);
+                bulk_load(sm.stage[c % 2].tab, ws + kWsTab, sizeof(sm.stage[0].tab), ch.full);
+            }
+            __syncwarp();
+        };
+        load(n - 1);
+        load_system(n - 1);
+        for (int c = n - 1; c >= 0; --c) {
+            cp_wait<0>();
+            tma_store_wait_read<0>();
+            fence_proxy_async_smem();
+            ch.failed |= !wait_products(ch.full, turn);
+            turn ^= 1;
+            if (__syncthreads_or(ch.failed)) break;
+            load(c - 1);
+            await<5>();
+            if (me == 0) {
+                bulk_store(chunk_ws(p, seq.slot + c, h) + kWsDS, sm.image, kImage);
+                tma_store_commit();
+            }
+            __syncwarp();
+            await<6>();  // T and P are used up
+            load_system(c - 1);
         }
-    for (int c = n - 1; c >= 0; --c) {
-        const StageB& st = sm.stage[c % 2];
-        float* const ws = chunk_ws(p, seq.slot + c, h);
-        const int t0 = c * kC;
-        float4 v[2], z[2], uu[2];
+        tma_store_wait_all<0>();
+    } else {  // ---- what lies between the products
+        const int half = warp / 4, row0 = warp % 4 * 32;
+        const Lane l;
+        float D[2][32];
+        const long long state = (static_cast<long long>(s) * p.H_v + h) * kD * kD;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = m0 + half * 8 + l.g, t = t0 + i;
-            v[half] = t < seq.len ? bf16x4(*reinterpret_cast<const uint2*>(p.V + p.v.at(s, seq.first + t, h) + v0)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            z[half] = *reinterpret_cast<const float4*>(ws + kWsZ + i * kD + v0);
-            uu[half] = *reinterpret_cast<const float4*>(ws + kWsU + i * kD + v0);
-        }
+        for (int lh = 0; lh < 2; ++lh)
+            for_pairs<32>([&](int row, int col, int i) {
+                const float2 x = p.dS_out == nullptr ? make_float2(0.f, 0.f)
+                                                     : *reinterpret_cast<const float2*>(p.dS_out + state + (row0 + lh * 16 + row) * kD + half * 64 + col);
+                D[lh][i] = x.x, D[lh][i + 1] = x.y;
+            });
+        for (int c = n - 1; c >= 0; --c) {
+            const StageB& st = sm.stage[c % 2];
+            float* const ws = chunk_ws(p, seq.slot + c, h);
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+            for (int lh = 0; lh < 2; ++lh) tm_st_split<16>(ch.tm + ch.lanes + (lh << 20) + kTmState + half * 32, 64, D[lh]);
+            publish();
+            if (__syncthreads_or(ch.failed)) break;
+            float2 u[2][8];
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-                *reinterpret_cast<float4*>(ws + kWsDS + (slice * kSlice + mt * 16 + half * 8 + l.g) * kD + warp * 16 + 4 * l.c) = pair_row(D[mt], half);
-        cp_wait<0>();
-        __syncthreads();
-        load(c - 1);
-        float y[2][4] = {}, x[2][4] = {};
+            for (int lh = 0; lh < 2; ++lh) {  // dO, its features on the lanes
+                uint32_t w[8];
+                turned(st.dO, half * 32, row0 + lh * 16, reinterpret_cast<uint32_t(&)[4]>(w[0]));
+                turned(st.dO, half * 32 + 16, row0 + lh * 16, reinterpret_cast<uint32_t(&)[4]>(w[4]));
+                tm_st_pairs(ch.tm + ch.lanes + (lh << 20) + kTmO + half * 16, w);
+            }
+            publish();
+            arrive<1>();
 #pragma unroll
-        for (int k0 = 0; k0 < kD; k0 += 8) {
-            float a[4], b[4];
-            a_rows(st.K, kLdX, m0, k0, l, a);
-            b_rows(sm.D, kLdN, n0, k0, l, b);
-            pair_b2(y, a, b);
-        }
-        for (int k0 = m0; k0 < kC; k0 += 8) {  // P^T dO: P is lower triangular
-            float a[4], b[4];
-            a_cols(st.P, kLdV, m0, k0, l, a);
-            b_cols(st.dO, kLdO, n0, k0, l, b);
-            pair_a2(x, a, b);
-        }
-        float dot_end[2];
+            for (int lh = 0; lh < 2; ++lh)
+                for_pairs<16>([&](int row, int col, int i) {
+                    u[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + half * 32 + col);
+                });
+            put_image(sm.image, D, row0, half);
+            fence_proxy_async_smem();
+            arrive<5>();
+            ch.wait();
+            float dots[kDots][8] = {};  // of this thread's eight tokens: 8 (i / 4) + 2 c + e at [i / 4 * 2 + e]
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = m0 + half * 8 + l.g;
-            const float4 e = scaled(pair_row(y, half), st.tab[TAB_ECK * kC + i]), q = pair_row(x, half);  // exp(g_C - g_i) D k_i
-            dot_end[half] = quad_sum(dot4(uu[half], e));
-            *reinterpret_cast<float4*>(sm.du + i * kLdS + n0 + 4 * l.c) = make_float4(e.x + q.x, e.y + q.y, e.z + q.z, e.w + q.w);
-            const float4 o = bf16x4(*reinterpret_cast<const uint2*>(st.dO + i * kLdO + n0 + 4 * l.c));
-            *reinterpret_cast<float4*>(sm.w + i * kLdS + n0 + 4 * l.c) = scaled(o, st.tab[TAB_SEGQ * kC + i]);
-        }
-        __syncthreads();
-        float r[2][4] = {};
-        for (int k0 = m0; k0 < kC; k0 += 8) {  // T^T is upper triangular
-            float a[4], b[4];
-            a_cols(st.T, kLdV, m0, k0, l, a);
-            b_cols(sm.du, kLdS, n0, k0, l, b);
-            pair_3(r, a, b);
-        }
+            for (int lh = 0; lh < 2; ++lh) {
+                float y[16], x[16];
+                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, y);
+                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmX + half * 32, x);
+                tmem_wait_ld();
+                for_pairs<16>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_ECK * kC + half * 32 + col);
+                    const float y0 = e.x * y[i], y1 = e.y * y[i + 1];
+                    dots[1][i / 4 * 2] = fmaf(u[lh][i / 2].x, y0, dots[1][i / 4 * 2]);
+                    dots[1][i / 4 * 2 + 1] = fmaf(u[lh][i / 2].y, y1, dots[1][i / 4 * 2 + 1]);
+                    x[i] += y0, x[i + 1] += y1;
+                });
+                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmDu + half * 16, 32, x);
+            }
+            publish();
+            arrive<2>();
+            float2 z[2][8];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = m0 + half * 8 + l.g;
-            const float4 e = pair_row(r, half);
-            *reinterpret_cast<float4*>(ws + kWsZ + i * kD + v0) = e;
-            *reinterpret_cast<float4*>(sm.w + (kC + i) * kLdS + n0 + 4 * l.c) = scaled(e, -st.tab[TAB_BEGK * kC + i]);
-            const float rz = quad_sum(dot4(e, z[half]));
-            const float rv = quad_sum(dot4(e, make_float4(v[half].x - z[half].x, v[half].y - z[half].y, v[half].z - z[half].z, v[half].w - z[half].w)));
-            if (l.c == 0) {
-                float(*const dots)[kC] = sm.dots[warp / 4];
-                dots[0][i] = rv, dots[1][i] = rz * st.tab[TAB_BETA * kC + i], dots[2][i] = dot_end[half];
+            for (int lh = 0; lh < 2; ++lh)
+                for_pairs<16>([&](int row, int col, int i) {
+                    z[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + half * 32 + col);
+                });
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float x[16];
+                uint32_t w[2][4];
+                turned(st.dO, half * 32, row0 + lh * 16, w[0]);
+                turned(st.dO, half * 32 + 16, row0 + lh * 16, w[1]);
+                for_pairs<16>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_SEGQ * kC + half * 32 + col);
+                    const uint32_t o = w[i / 8][i % 8 / 2];
+                    x[i] = e.x * bf16_lo(o), x[i + 1] = e.y * bf16_hi(o);
+                });
+                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmW + half * 16, 32, x);
+            }
+            publish();
+            arrive<3>();
+            ch.wait();  // (for r; what was issued behind it may still run)
+            arrive<6>();
+            float r[2][16];
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float x[16];
+                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, r[lh]);
+                tmem_wait_ld();
+                for_pairs<16>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_BEGK * kC + half * 32 + col);
+                    x[i] = -e.x * r[lh][i], x[i + 1] = -e.y * r[lh][i + 1];
+                });
+                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmDu + half * 16, 32, x);
+            }
+            publish();
+            arrive<4>();
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh)
+                for_pairs<16>([&](int row, int col, int i) {
+                    dots[0][i / 4 * 2] = fmaf(r[lh][i], z[lh][i / 2].x, dots[0][i / 4 * 2]);
+                    dots[0][i / 4 * 2 + 1] = fmaf(r[lh][i + 1], z[lh][i / 2].y, dots[0][i / 4 * 2 + 1]);
+                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + half * 32 + col) = make_float2(r[lh][i], r[lh][i + 1]);
+                });
+            // the tokens' sums over this warp's 32 features: lanes of one column group trade halves of their tokens
+#pragma unroll
+            for (int d = 0; d < kDots; ++d) {
+                float a[4], b[2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float keep = l.g & 4 ? dots[d][4 + i] : dots[d][i], give = l.g & 4 ? dots[d][i] : dots[d][4 + i];
+                    a[i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float keep = l.g & 2 ? a[2 + i] : a[i], give = l.g & 2 ? a[i] : a[2 + i];
+                    b[i] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+                }
+                const float keep = l.g & 1 ? b[1] : b[0], give = l.g & 1 ? b[0] : b[1];
+                // (the bits of l.g are those of the token's place)
+                sm.dots[warp % 4][d][half * 32 + (l.g >> 1) * 8 + 2 * l.c + (l.g & 1)] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
+            }
+            const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
+            asm volatile("bar.sync 7, %0;" ::"n"(kThreads) : "memory");
+            if (threadIdx.x < kDots * kC) {
+                const float* const at = &sm.dots[0][0][threadIdx.x];
+                ws[kWsDots + threadIdx.x] = (at[0] + at[kDots * kC]) + (at[2 * kDots * kC] + at[3 * kDots * kC]);
+            }
+            ch.wait();
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float x[32];
+                tm_ld64(ch.tm + ch.lanes + (lh << 20) + kTmDelta + half * 64, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) D[lh][i] = fmaf(decay, D[lh][i], x[i]);
             }
         }
-        __syncthreads();
-        if (tid < kDots * kC) ws[kWsDots + slice * kDots * kC + tid] = sm.dots[0][tid / kC][tid % kC] + sm.dots[1][tid / kC][tid % kC];
-        const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
+        if (p.dS_in != nullptr) {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            float d[2][4] = {};
-#pragma unroll
-            for (int k0 = 0; k0 < kC; k0 += 8) {
-                float a[4], b[4];
-                a_cols(sm.w, kLdS, mt * 16, k0, l, a);
-                b_cols(st.Q, kLdX, warp * 16, k0, l, b);
-                pair_a2(d, a, b);
-                a_cols(sm.w + kC * kLdS, kLdS, mt * 16, k0, l, a);
-                b_cols(st.K, kLdX, warp * 16, k0, l, b);
-                pair_a2(d, a, b);
-            }
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) D[mt][q][e] = fmaf(decay, D[mt][q][e], d[q][e]);
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-                *reinterpret_cast<float4*>(sm.D + (mt * 16 + half * 8 + l.g) * kLdN + warp * 16 + 4 * l.c) = pair_row(D[mt], half);
+            for (int lh = 0; lh < 2; ++lh)
+                for_pairs<32>([&](int row, int col, int i) {
+                    *reinterpret_cast<float2*>(p.dS_in + state + (row0 + lh * 16 + row) * kD + half * 64 + col) = make_float2(D[lh][i], D[lh][i + 1]);
+                });
         }
     }
-    if (p.dS_in != nullptr) {
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-                *reinterpret_cast<float4*>(p.dS_in + state + (mt * 16 + half * 8 + l.g) * kD + warp * 16 + 4 * l.c) = pair_row(D[mt], half);
-    }
+    chain_end(ch, p.status, kTmColumns);
 }
 
 // ---------------------------------------------------------------- the chunks' gradients
-struct SmemC {
-    __nv_bfloat16 K[kC * kLdX], Q[kC * kLdX], dO[kC * kLdX];
-    float u[kC * kLdF], r[kC * kLdF];
-    union {
-        float S[kD * kLdN];  // the state, then its gradient
-        struct {
-            float p[kC * kLdV], m[kC * kLdM];
-        } pair;
-    };
-    float tab[kTabs * kC];
-    float rowq[4][kC], rown[2][kC], rowb[2][kC], coln[4][kC];
-    float ds[kThreads / 32];
-};
+// One CTA has a (chunk, key head) and takes the value heads that share it in turn. dQ and dK are summed transposed, a key feature on each of the
+// 128 lanes: A is S or D (tiles [v][key], read down the rows) or K or Q (read down the rows), B is dO, r, u, p or m (64 tokens wide). p and m
+// come from products of 64 x 64 (rows on 16 lanes of every quarter), r and u in three pieces: dbeta and dg are made of them. S and D have two
+// pieces (2^-17), which dQ and dK do not notice and dg hardly: <D, S> and <q, S^T dO>. What bounds it: the 304 KB that a value head's chunk reads and
+// writes (5.8 us of an SM's share of the HBM); the products take 150 issues of 32 cycles, 2.5 us.
+constexpr int kGradThreads = 512;  // 16 warps, and one that issues the products and the copies of S and D
 
-__global__ void __launch_bounds__(kThreads) chunk_grads_kernel(const ParamsB p) {
+struct SmemC {
+    uint8_t K[2 * kTile], Q[2 * kTile], dO[2 * kTile];
+    uint8_t S[kImage];                                     // the state, then its gradient; at the end dQ and dK on their way out
+    uint8_t u[kPieces][2 * kTile], r[kPieces][2 * kTile];  // [v][token]; in the place of the third pieces, p and m: two pieces each
+    float tab[kTabs * kC];
+    float rowq[4][kC], rown[4][kC], rowb[4][kC], coln[4][kC], rv[2][kC];
+    float ds[kGradThreads / 32];
+};
+static_assert(2 * kC * kLdX * 2 <= kImage, "");
+
+__device__ __forceinline__ void tm_ld16(uint32_t taddr, float (&x)[8]) {  // 16 lanes x 16 columns
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void ldmatrix_turned(uint32_t at, uint32_t (&w)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+}
+// `turned` from a tile pair in the 128-byte swizzle
+__device__ __forceinline__ void turned_swizzled(const uint8_t* tile, int t0, int v0, uint32_t (&w)[4]) {
+    const int lane = threadIdx.x % 32, t = t0 + (lane & 7) + (lane >> 4) * 8, v = v0 + ((lane >> 3) & 1) * 8;
+    ldmatrix_turned(smem_u32(tile + v / 64 * kTile + swizzled(t, v % 64)), w);
+}
+// the sum over the lanes of a column group of four tokens' values; a lane gets that of token place l.g / 2
+__device__ __forceinline__ float token_sum(const float (&x)[4], const Lane& l) {
+    float a[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float keep = l.g & 4 ? x[2 + i] : x[i], give = l.g & 4 ? x[i] : x[2 + i];
+        a[i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+    }
+    const float keep = l.g & 2 ? a[1] : a[0], give = l.g & 2 ? a[0] : a[1];
+    const float b = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+    return b + __shfl_xor_sync(0xffffffffu, b, 4);
+}
+template <int ID>
+__device__ __forceinline__ void grad_arrive() {
+    asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kGradThreads + 32) : "memory");
+}
+template <int ID>
+__device__ __forceinline__ void grad_await() {
+    asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kGradThreads + 32) : "memory");
+}
+__device__ __forceinline__ void grad_sync() { asm volatile("bar.sync 5, %0;" ::"n"(kGradThreads) : "memory"); }
+
+// N products over K in steps of 16: A and B advance by their steps (bytes); `half_a`, `half_b`: extra step behind every 64
+template <int N>
+__device__ __forceinline__ void product(uint32_t d, uint64_t a, int step_a, uint64_t b, int step_b, uint32_t idesc, bool more) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int ka = step_a == 32 ? (k >> 2) * kTile + (k & 3) * 32 : k * step_a, kb = step_b == 32 ? (k >> 2) * kTile + (k & 3) * 32 : k * step_b;
+        mma_f16_ss(d, a + ka / 16, b + kb / 16, idesc, more || k > 0);
+    }
+}
+constexpr int kAlong = 32, kDown = 2048;  // steps of an operand whose sum index runs along the rows, down the rows
+__host__ __device__ constexpr uint32_t grad_idesc(int m, bool a_down, bool b_down, bool minus) {
+    return instr_desc(m, 64, 1, 1, a_down, b_down, 1) | (minus ? kNegA : 0u);
+}
+constexpr uint32_t kTmDOS = 0, kTmRS = 64, kTmUD = 128, kTmDQ = 192, kTmDK = 256, kTmOU = 320, kTmRU = 384, kTmKK = kTmDQ, kTmQK = kTmDK;
+
+__global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const ParamsB p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    SmemC& sm = *reinterpret_cast<SmemC*>(smem_raw);
+    SmemC& sm = *reinterpret_cast<SmemC*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
+    __shared__ uint64_t bar_pair, bar_s, bar_out, bar_d, bar_load;
+    __shared__ uint32_t base;
     const int hk = blockIdx.x % p.H_k, slot = blockIdx.x / p.H_k;
     int s, first, rows;
     if (!chunk_of(p, slot, s, first, rows)) return;
     const int tid = threadIdx.x, warp = tid / 32;
     const Lane l;
-    copy_rows<kLdX, kD>(sm.K, p.K + p.qk.at(s, first, hk), p.qk.token, rows);
-    copy_rows<kLdX, kD>(sm.Q, p.Q + p.qk.at(s, first, hk), p.qk.token, rows);
-    // tokens x features: 32 x 32 a warp, two pairs of tiles wide; tokens x tokens: 16 x 32 a warp
-    const int wm = warp % 2 * 32, wn = warp / 2 * 32;
-    const int pm = warp % 4 * 16, pn = warp / 4 * 32;
-    float dq[2][2][2][4] = {}, dk[2][2][2][4] = {};  // [rows][pair][tile][], times 1 / ||q||, 1 / ||k||
-    const auto add_scaled = [&](float (&to)[2][2][2][4], const float (&x)[2][2][2][4], const float* tab, float sign) {
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            const float e0 = sign * tab[wm + mt * 16 + l.g], e1 = sign * tab[wm + mt * 16 + 8 + l.g];
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    to[mt][q][t][0] = fmaf(e0, x[mt][q][t][0], to[mt][q][t][0]);
-                    to[mt][q][t][1] = fmaf(e0, x[mt][q][t][1], to[mt][q][t][1]);
-                    to[mt][q][t][2] = fmaf(e1, x[mt][q][t][2], to[mt][q][t][2]);
-                    to[mt][q][t][3] = fmaf(e1, x[mt][q][t][3], to[mt][q][t][3]);
+    bool failed = false;
+    if (tid == 0) {
+        for (uint64_t* b : {&bar_pair, &bar_s, &bar_out, &bar_d, &bar_load}) mbar_init(b, 1);
+        mbar_fence_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(&base, kTmColumns);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tm = base;
+    const int heads = p.group;
+
+    if (warp == kGradThreads / 32) {  // ---- products and the copies of S and D
+        const uint32_t K = smem_u32(sm.K), Q = smem_u32(sm.Q), dO = smem_u32(sm.dO), S = smem_u32(sm.S);
+        const auto tile_u = [&](int i) { return smem_u32(sm.u[i]); };
+        const auto tile_r = [&](int i) { return smem_u32(sm.r[i]); };
+        const auto state = [&](int i) { return smem_desc(S + i * (kImage / 2), 2 * kTile, 1024, SWZ_128B); };
+        uint32_t loads = 0;
+        for (int it = 0; it < heads; ++it) {
+            const int hv = hk * heads + it;
+            float* const ws = chunk_ws(p, slot, hv);
+            const auto load = [&](const float* from) {
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&bar_load, kImage);
+                    bulk_load(sm.S, from, kImage, &bar_load);
                 }
-        }
-    };
-    // rows of `x` times rows of a bf16 tile: this thread's share of row i, summed over the lanes of the row
-    const auto row_dot = [&](const float (&x)[2][2][2][4], const __nv_bfloat16* tile, int mt, int half) {
-        const int i = wm + mt * 16 + half * 8 + l.g;
-        float d = 0.f;
+                __syncwarp();
+            };
+            load(ws + kWsS);
+            grad_await<1>();  // K, Q, dO, u, r are there
+            tc_fence_after_sync();
+            if (elect_one()) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) d += dot4(pair_row(x[mt][q], half), bf16x4(*reinterpret_cast<const uint2*>(tile + i * kLdX + wn + q * 16 + 4 * l.c)));
-        return quad_sum(d);
-    };
-    for (int hv = hk * p.group; hv < (hk + 1) * p.group; ++hv) {
-        const float* const ws = chunk_ws(p, slot, hv);
-        copy_rows<kLdX, kD>(sm.dO, p.dO + p.v.at(s, first, hv), p.v.token, rows);
-        copy_floats<kLdF, kC, kD>(sm.u, ws + kWsU, kD);
-        copy_floats<kLdF, kC, kD>(sm.r, ws + kWsZ, kD);
-        copy_floats<kLdN, kD, kD>(sm.S, ws + kWsS, kD);
-        copy_floats<kTabs * kC, 1, kTabs * kC>(sm.tab, ws + kWsTab, 0);
-        cp_commit();
-        cp_wait<0>();
-        __syncthreads();
-        const float decay = expf(sm.tab[TAB_G * kC + kC - 1]);
-        {  // dO S (two products: <q, S^T dO> is part of dg) and r S
-            float x[2][2][2][4] = {}, w[2][2][2][4] = {};
-#pragma unroll 2
-            for (int k0 = 0; k0 < kD; k0 += 8) {
-                float o[2][4], r[2][4];
+                for (int i = kPieces - 1; i >= 0; --i)
+                    product<8>(tm + kTmOU, desc_rows(dO), kAlong, desc_cols(tile_u(i)), kDown, grad_idesc(64, false, true, i == 1), i < kPieces - 1);
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
-                    a_rows(sm.dO, kLdX, wm + mt * 16, k0, l, o[mt]);
-                    a_rows(sm.r, kLdF, wm + mt * 16, k0, l, r[mt]);
-                }
+                for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float b[4], hi[4], lo[4];
-                    b_cols(sm.S, kLdN, wn + q * 16, k0, l, b);
-                    split(b, hi, lo);
-#pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) {
-                        pair_1(x[mt][q], o[mt], lo);
-                        pair_1(x[mt][q], o[mt], hi);
-                        pair_1(w[mt][q], r[mt], b);
-                    }
-                }
+                    for (int i = sum; i >= 0; --i)
+                        product<8>(tm + kTmRU, desc_cols(tile_r(i)), kDown, desc_cols(tile_u(sum - i)), kDown,
+                                   grad_idesc(64, true, true, (i == 1) != (sum - i == 1)), sum < 2 || i < 2);
+                product<8>(tm + kTmKK, desc_rows(K), kAlong, desc_rows(K), kAlong, grad_idesc(64, false, false, false), false);
+                product<8>(tm + kTmQK, desc_rows(Q), kAlong, desc_rows(K), kAlong, grad_idesc(64, false, false, false), false);
+                mma_commit(&bar_pair);
             }
-            float part[2][2][2][4] = {};
-            add_scaled(part, x, sm.tab + TAB_SEGQ * kC, 1.f);
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float d = row_dot(part, sm.Q, mt, half);
-                    if (l.c == 0) sm.rowq[warp / 2][wm + mt * 16 + half * 8 + l.g] = d;
-                }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) (&dq[0][0][0][0])[i] += (&part[0][0][0][0])[i];
-            add_scaled(dk, w, sm.tab + TAB_BEGK * kC, -1.f);
-        }
-        __syncthreads();
-        {  // the state's gradient in the state's place, and their product
-            float d = 0.f;
-            for (int i = tid; i < kD * kD / 4; i += kThreads) {
-                float4* const at = reinterpret_cast<float4*>(sm.S + (i / 32) * kLdN + i % 32 * 4);
-                const float4 x = *reinterpret_cast<const float4*>(ws + kWsDS + i * 4);
-                d += dot4(*at, x);
-                *at = x;
+            __syncwarp();
+            failed |= !wait_products(&bar_load, loads++ & 1);
+            if (elect_one()) {
+                product<8>(tm + kTmDOS, state(1), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, true), false);
+                product<8>(tm + kTmDOS, state(0), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, false), true);
+                product<8>(tm + kTmRS, state(1), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, true), false);
+                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(1)), kDown, grad_idesc(128, true, true, true), true);
+                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, false), true);
+                mma_commit(&bar_s);
             }
-            for (int o = 16; o > 0; o /= 2) d += __shfl_xor_sync(0xffffffffu, d, o);
-            if (tid % 32 == 0) sm.ds[warp] = d;
-        }
-        __syncthreads();
-        {  // u D
-            float x[2][2][2][4] = {};
-#pragma unroll 2
-            for (int k0 = 0; k0 < kD; k0 += 8) {
-                float a[2][4];
+            __syncwarp();
+            grad_await<2>();  // p, m
+            tc_fence_after_sync();
+            if (elect_one()) {
+                const uint64_t Kd = desc_cols(K), Qd = desc_cols(Q);
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt) a_rows(sm.u, kLdF, wm + mt * 16, k0, l, a[mt]);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float b[4];
-                    b_cols(sm.S, kLdN, wn + q * 16, k0, l, b);
-#pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) pair_1(x[mt][q], a[mt], b);
+                for (int i = 1; i >= 0; --i) {
+                    const uint32_t pt = tile_u(2) + i * kTile, mt = tile_r(2) + i * kTile;
+                    product<4>(tm + kTmDQ, Kd, kDown, desc_rows(pt), kAlong, grad_idesc(128, true, false, i == 1), i == 0);
+                    product<4>(tm + kTmDK, Qd, kDown, desc_cols(pt), kDown, grad_idesc(128, true, true, i == 1), i == 0);
+                    product<4>(tm + kTmDK, Kd, kDown, desc_rows(mt), kAlong, grad_idesc(128, true, false, i == 1), true);
+                    product<4>(tm + kTmDK, Kd, kDown, desc_cols(mt), kDown, grad_idesc(128, true, true, i == 1), true);
                 }
+                mma_commit(&bar_out);
             }
-            add_scaled(dk, x, sm.tab + TAB_ECK * kC, 1.f);
-        }
-        __syncthreads();
-        {  // dO u^T, r u^T, k k^T, q k^T; what they make
-            float ou[4][4] = {}, ru[4][4] = {}, kk[4][4] = {}, qk[4][4] = {};
-#pragma unroll 2
-            for (int k0 = 0; k0 < kD; k0 += 16) {
-                const auto word = [&](const __nv_bfloat16* x, int row, int k) { return *reinterpret_cast<const uint32_t*>(x + row * kLdX + k + 2 * l.c); };
-                const uint32_t ak[4] = {word(sm.K, pm + l.g, k0), word(sm.K, pm + l.g + 8, k0), word(sm.K, pm + l.g, k0 + 8), word(sm.K, pm + l.g + 8, k0 + 8)};
-                const uint32_t aq[4] = {word(sm.Q, pm + l.g, k0), word(sm.Q, pm + l.g + 8, k0), word(sm.Q, pm + l.g, k0 + 8), word(sm.Q, pm + l.g + 8, k0 + 8)};
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const uint32_t b0 = word(sm.K, pn + n * 8 + l.g, k0), b1 = word(sm.K, pn + n * 8 + l.g, k0 + 8);
-                    mma_bf16(kk[n], ak, b0, b1);
-                    mma_bf16(qk[n], aq, b0, b1);
-                }
-#pragma unroll
-                for (int k1 = k0; k1 < k0 + 16; k1 += 8) {
-                    float o[4], r[4], rh[4], rl[4];
-                    a_rows(sm.dO, kLdX, pm, k1, l, o);
-                    a_rows(sm.r, kLdF, pm, k1, l, r);
-                    split(r, rh, rl);
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const float2 b = *reinterpret_cast<const float2*>(sm.u + (pn + n * 8 + l.g) * kLdF + k1 + 2 * l.c);
-                        const float h0 = tf_hi(b.x), h1 = tf_hi(b.y), l0 = b.x - h0, l1 = b.y - h1;
-                        mma_tf32(ou[n], o, l0, l1);
-                        mma_tf32(ou[n], o, h0, h1);
-                        mma_tf32(ru[n], rl, h0, h1);
-                        mma_tf32(ru[n], rh, l0, l1);
-                        mma_tf32(ru[n], rh, h0, h1);
-                    }
-                }
+            __syncwarp();
+            grad_await<3>();  // the state is used up
+            load(ws + kWsDS);
+            failed |= !wait_products(&bar_load, loads++ & 1);
+            if (elect_one()) {
+                product<8>(tm + kTmUD, state(1), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, true), false);
+                product<8>(tm + kTmUD, state(0), kDown, desc_cols(tile_u(1)), kDown, grad_idesc(128, true, true, true), true);
+                product<8>(tm + kTmUD, state(0), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, false), true);
+                mma_commit(&bar_d);
             }
-            const float* const g = sm.tab + TAB_G * kC;
-            const float* const rk = sm.tab + TAB_RK * kC;
-            float rown[2] = {}, rowb[2] = {};
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                float coln[2] = {};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = pm + l.g + (e / 2) * 8, j = pn + n * 8 + 2 * l.c + e % 2;
-                    const float gam = j <= i ? expf(g[i] - g[j]) : 0.f;
-                    const float rr = rk[i] * rk[j];
-                    const float qq = p.scale * gam * sm.tab[TAB_RQ * kC + i] * rk[j];
-                    // p_ij and m_ij with the lengths of the rows that they will multiply
-                    const float pp = j <= i ? ou[n][e] * qq : 0.f;
-                    const float kg = j < i ? -gam * rr * ru[n][e] : 0.f, mm = sm.tab[TAB_BETA * kC + i] * kg;
-                    const float both = j < i ? fmaf(pp, qk[n][e], mm * kk[n][e]) : 0.f;
-                    rown[e / 2] += both;
-                    coln[e % 2] += both;
-                    if (j < i) rowb[e / 2] = fmaf(kg, kk[n][e], rowb[e / 2]);
-                    sm.pair.p[i * kLdV + j] = pp;
-                    if (j < i) {
-                        sm.pair.m[i * kLdM + j] = mm;
-                        sm.pair.m[j * kLdM + i] = mm;
-                    } else if (j == i) {
-                        sm.pair.m[i * kLdM + i] = 0.f;
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int o = 4; o < 32; o *= 2) coln[e] += __shfl_xor_sync(0xffffffffu, coln[e], o);
-                    if (l.g == 0) sm.coln[warp % 4][pn + n * 8 + 2 * l.c + e] = coln[e];
-                }
-            }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const float a = quad_sum(rown[half]), b = quad_sum(rowb[half]);
-                if (l.c == 0) sm.rown[warp / 4][pm + half * 8 + l.g] = a, sm.rowb[warp / 4][pm + half * 8 + l.g] = b;
-            }
-        }
-        __syncthreads();
-        for (int k0 = 0; k0 < kC; k0 += 8) {  // p k, p^T q, (m + m^T) k
-            float bk[2][4], bq[2][4];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                b_cols(sm.K, kLdX, wn + q * 16, k0, l, bk[q]);
-                b_cols(sm.Q, kLdX, wn + q * 16, k0, l, bq[q]);
-            }
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-                float a[4];
-                if (k0 <= wm + mt * 16 + 15) {
-                    a_rows(sm.pair.p, kLdV, wm + mt * 16, k0, l, a);
-                    pair_1(dq[mt][0], a, bk[0]);
-                    pair_1(dq[mt][1], a, bk[1]);
-                }
-                if (k0 + 7 >= wm + mt * 16) {
-                    a_cols(sm.pair.p, kLdV, wm + mt * 16, k0, l, a);
-                    pair_1(dk[mt][0], a, bq[0]);
-                    pair_1(dk[mt][1], a, bq[1]);
-                }
-                a_rows(sm.pair.m, kLdM, wm + mt * 16, k0, l, a);
-                pair_1(dk[mt][0], a, bk[0]);
-                pair_1(dk[mt][1], a, bk[1]);
-            }
-        }
-        // dV = beta r
-        for (int i = tid; i < kC * kD / 8; i += kThreads) {
-            const int row = i / (kD / 8), col = i % (kD / 8) * 8;
-            if (row < rows) {
-                const float b = sm.tab[TAB_BETA * kC + row];
-                const float4 x = scaled(*reinterpret_cast<const float4*>(sm.r + row * kLdF + col), b), y = scaled(*reinterpret_cast<const float4*>(sm.r + row * kLdF + col + 4), b);
-                *reinterpret_cast<uint4*>(p.dV + p.v.at(s, first + row, hv) + col) =
-                    make_uint4(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w), pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
-            }
-        }
-        if (warp == 0) {  // dbeta, dg: lane i has tokens 2i, 2i + 1
+            __syncwarp();
+            grad_await<4>();  // every part of dbeta and dg. Lane i has tokens 2i, 2i + 1
+            const int lane = tid % 32;
             float d[2], ends = 0.f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int i = 2 * tid + e;
-                float direct = 0.f, rz = 0.f, end = 0.f;
-#pragma unroll
-                for (int x = 0; x < kSlices; ++x) {
-                    const float* const dots = ws + kWsDots + x * kDots * kC;
-                    direct += dots[i], rz += dots[kC + i], end += dots[2 * kC + i];
-                }
-                if (i < rows) p.dbeta[p.gate.at(s, first + i, hv)] = direct + sm.rowb[0][i] + sm.rowb[1][i];
-                d[e] = sm.rown[0][i] + sm.rown[1][i] - (sm.coln[0][i] + sm.coln[1][i] + sm.coln[2][i] + sm.coln[3][i]) +
-                       (sm.rowq[0][i] + sm.rowq[1][i] + sm.rowq[2][i] + sm.rowq[3][i]) - rz - end;
+                const int i = 2 * lane + e;
+                const float rz = ws[kWsDots + i], end = ws[kWsDots + kC + i];
+                const float sums[4] = {(sm.rown[0][i] + sm.rown[1][i]) + (sm.rown[2][i] + sm.rown[3][i]), (sm.rowb[0][i] + sm.rowb[1][i]) + (sm.rowb[2][i] + sm.rowb[3][i]),
+                                       (sm.coln[0][i] + sm.coln[1][i]) + (sm.coln[2][i] + sm.coln[3][i]), (sm.rowq[0][i] + sm.rowq[1][i]) + (sm.rowq[2][i] + sm.rowq[3][i])};
+                if (i < rows) p.dbeta[p.gate.at(s, first + i, hv)] = (sm.rv[0][i] + sm.rv[1][i]) - rz + sums[1];
+                d[e] = sums[0] - sums[2] + sums[3] - sm.tab[TAB_BETA * kC + i] * rz - end;
                 ends += end;
             }
 #pragma unroll
             for (int o = 16; o > 0; o /= 2) ends += __shfl_xor_sync(0xffffffffu, ends, o);
             float dsum = 0.f;
 #pragma unroll
-            for (int x = 0; x < kThreads / 32; ++x) dsum += sm.ds[x];
-            if (tid == 31) d[1] += ends + decay * dsum;
+            for (int x = 0; x < kGradThreads / 32; ++x) dsum += sm.ds[x];
+            if (lane == 31) d[1] += ends + expf(sm.tab[TAB_G * kC + kC - 1]) * dsum;
             float sum = d[0] + d[1];
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
                 const float x = __shfl_down_sync(0xffffffffu, sum, o);
-                if (tid + o < 32) sum += x;
+                if (lane + o < 32) sum += x;
             }
-            if (2 * tid < rows) p.dg[p.gate.at(s, first + 2 * tid, hv)] = sum;
-            if (2 * tid + 1 < rows) p.dg[p.gate.at(s, first + 2 * tid + 1, hv)] = sum - d[0];
-        }
-        __syncthreads();
-    }
-    // through the norm of the rows: x - ||row||^-2 <row, x> row
-    const auto finish = [&](const float (&x)[2][2][2][4], const __nv_bfloat16* tile, const float* inv, __nv_bfloat16* out) {
-        if (p.l2norm) {
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float d = row_dot(x, tile, mt, half);
-                    if (l.c == 0) sm.rowq[warp / 2][wm + mt * 16 + half * 8 + l.g] = d;
-                }
+            if (2 * lane < rows) p.dg[p.gate.at(s, first + 2 * lane, hv)] = sum;
+            if (2 * lane + 1 < rows) p.dg[p.gate.at(s, first + 2 * lane + 1, hv)] = sum - d[0];
             __syncthreads();
         }
+        __syncthreads();
+        __syncthreads();
+    } else {
+        const int quad = warp % 4, quarter = warp / 4;  // 32 key features (16 tokens of p, m), 16 tokens
+        const uint32_t lanes = tm + (static_cast<uint32_t>(quad * 32) << 16) + quarter * 16;
+        const int t0 = quarter * 16 + 2 * l.c;  // this thread's tokens: t0, t0 + 1, t0 + 8, t0 + 9
+        float dq[2][8] = {}, dk[2][8] = {};     // [16 lanes][see for_pairs], times 1 / ||q||, 1 / ||k||
+        copy_tile<kGradThreads>(sm.K, p.K + p.qk.at(s, first, hk), p.qk.token, rows, tid);
+        copy_tile<kGradThreads>(sm.Q, p.Q + p.qk.at(s, first, hk), p.qk.token, rows, tid);
+        // a token's sum over the features of x times K or Q, in four parts
+        const auto put_dots = [&](const float (&x)[2][8], const uint8_t* tile, float (*to)[kC]) {
+            float d[4] = {};
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+            for (int lh = 0; lh < 2; ++lh) {
+                uint32_t w[4];
+                turned_swizzled(tile, quarter * 16, quad * 32 + lh * 16, w);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int i = wm + mt * 16 + half * 8 + l.g;
-                const float d = p.l2norm ? inv[i] * inv[i] * (sm.rowq[0][i] + sm.rowq[1][i] + sm.rowq[2][i] + sm.rowq[3][i]) : 0.f;
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int col = wn + q * 16 + 4 * l.c;
-                    const float4 a = pair_row(x[mt][q], half), b = bf16x4(*reinterpret_cast<const uint2*>(tile + i * kLdX + col));
-                    if (i < rows)
-                        *reinterpret_cast<uint2*>(out + p.qk.at(s, first + i, hk) + col) =
-                            make_uint2(pack_bf16x2(a.x - d * b.x, a.y - d * b.y), pack_bf16x2(a.z - d * b.z, a.w - d * b.w));
+                for (int i = 0; i < 8; i += 2) {
+                    d[i / 4 * 2] = fmaf(x[lh][i], bf16_lo(w[i / 2]), d[i / 4 * 2]);
+                    d[i / 4 * 2 + 1] = fmaf(x[lh][i + 1], bf16_hi(w[i / 2]), d[i / 4 * 2 + 1]);
                 }
             }
+            const float sum = token_sum(d, l);
+            if ((l.g & 1) == 0) to[quad][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
+        };
+        for (int it = 0; it < heads; ++it) {
+            const int hv = hk * heads + it;
+            const uint32_t turn = it & 1;
+            const float* const ws = chunk_ws(p, slot, hv);
+            copy_tile<kGradThreads>(sm.dO, p.dO + p.v.at(s, first, hv), p.v.token, rows, tid);
+            for (int i = tid * 4; i < kTabs * kC; i += kGradThreads * 4) cp16(sm.tab + i, ws + kWsTab + i, true);
+            cp_commit();
+            {  // u and r in pieces
+                float4 x[2][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[0][i] = reinterpret_cast<const float4*>(ws + kWsU)[tid + i * kGradThreads];
+                    x[1][i] = reinterpret_cast<const float4*>(ws + kWsZ)[tid + i * kGradThreads];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = tid + i * kGradThreads, place = swizzled(at / 16, at % 16 * 4);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        uint32_t w[kPieces][2];
+                        split3(x[t][i].x, x[t][i].y, w[0][0], w[1][0], w[2][0]);
+                        split3(x[t][i].z, x[t][i].w, w[0][1], w[1][1], w[2][1]);
+#pragma unroll
+                        for (int q = 0; q < kPieces; ++q) *reinterpret_cast<uint2*>((t ? sm.r : sm.u)[q] + place) = make_uint2(w[q][0], w[q][1]);
+                    }
+                }
+            }
+            cp_wait<0>();
+            fence_proxy_async_smem();
+            grad_arrive<1>();
+            grad_sync();
+            {  // dV = beta r, turned back, and <r, v>
+                const int t = warp % 8 * 8, v0 = warp / 8 * 64, row = t + l.g;
+                const float b = sm.tab[TAB_BETA * kC + row];
+                const long long at = p.v.at(s, first + row, hv) + v0 + 2 * l.c;
+                float rv = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t w[kPieces][4];
+                    const int v = v0 + i * 32 + tid % 32;
+#pragma unroll
+                    for (int q = 0; q < kPieces; ++q) ldmatrix_turned(smem_u32(sm.r[q] + swizzled(v, t)), w[q]);
+                    if (row < rows) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float x = (bf16_lo(w[0][k]) - bf16_lo(w[1][k])) + bf16_lo(w[2][k]), y = (bf16_hi(w[0][k]) - bf16_hi(w[1][k])) + bf16_hi(w[2][k]);
+                            const uint32_t vv = *reinterpret_cast<const uint32_t*>(p.V + at + i * 32 + k * 8);
+                            rv = fmaf(x, bf16_lo(vv), fmaf(y, bf16_hi(vv), rv));
+                            *reinterpret_cast<uint32_t*>(p.dV + at + i * 32 + k * 8) = pack_bf16x2(b * x, b * y);
+                        }
+                    }
+                }
+                rv = quad_sum(rv);
+                if (l.c == 0) sm.rv[warp / 8][row] = rv;
+            }
+            grad_sync();  // the third pieces make room
+            failed |= !wait_products(&bar_pair, turn);
+            tc_fence_after_sync();
+            {  // p, m, and what dbeta and dg have of them
+                float ou[8], ru[8], kk[8], qk[8];
+                tm_ld16(lanes + kTmOU, ou);
+                tm_ld16(lanes + kTmRU, ru);
+                tm_ld16(lanes + kTmKK, kk);
+                tm_ld16(lanes + kTmQK, qk);
+                tmem_wait_ld();
+                const float* const g = sm.tab + TAB_G * kC;
+                const float* const rk = sm.tab + TAB_RK * kC;
+                float rown[2] = {}, rowb[2] = {}, coln[4] = {};
+#pragma unroll
+                for (int x = 0; x < 8; x += 2) {
+                    const int i = quad * 16 + ((x >> 1) & 1) * 8 + l.g, j0 = t0 + (x >> 2) * 8;
+                    float pp[2], mm[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int j = j0 + e;
+                        const float gam = j <= i ? expf(g[i] - g[j]) * rk[j] : 0.f;
+                        // p_ij and m_ij with the lengths of the rows that they will multiply
+                        pp[e] = j <= i ? ou[x + e] * (p.scale * gam * sm.tab[TAB_RQ * kC + i]) : 0.f;
+                        const float kg = j < i ? -gam * rk[i] * ru[x + e] : 0.f;
+                        mm[e] = sm.tab[TAB_BETA * kC + i] * kg;
+                        if (j < i) {
+                            const float both = fmaf(pp[e], qk[x + e], mm[e] * kk[x + e]);
+                            rown[(x >> 1) & 1] += both;
+                            coln[(x >> 2) * 2 + e] += both;
+                            rowb[(x >> 1) & 1] = fmaf(kg, kk[x + e], rowb[(x >> 1) & 1]);
+                        }
+                    }
+                    const int place = swizzled(i, j0);
+                    uint32_t h = pack_bf16x2(pp[0], pp[1]);
+                    *reinterpret_cast<uint32_t*>(sm.u[2] + place) = h;
+                    *reinterpret_cast<uint32_t*>(sm.u[2] + kTile + place) = pack_bf16x2(bf16_minus_lo(h, pp[0]), bf16_minus_hi(h, pp[1]));
+                    h = pack_bf16x2(mm[0], mm[1]);
+                    *reinterpret_cast<uint32_t*>(sm.r[2] + place) = h;
+                    *reinterpret_cast<uint32_t*>(sm.r[2] + kTile + place) = pack_bf16x2(bf16_minus_lo(h, mm[0]), bf16_minus_hi(h, mm[1]));
+                }
+                fence_proxy_async_smem();
+                tc_fence_before_sync();
+                grad_arrive<2>();
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float a = quad_sum(rown[e]), b = quad_sum(rowb[e]);
+                    if (l.c == 0) sm.rown[quarter][quad * 16 + e * 8 + l.g] = a, sm.rowb[quarter][quad * 16 + e * 8 + l.g] = b;
+                }
+                const float sum = token_sum(coln, l);
+                if ((l.g & 1) == 0) sm.coln[quad][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
+            }
+            failed |= !wait_products(&bar_load, 0);
+            failed |= !wait_products(&bar_s, turn);
+            tc_fence_after_sync();
+            uint4 x[2][4];
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[q][i] = *reinterpret_cast<const uint4*>(sm.S + q * (kImage / 2) + (tid + i * kGradThreads) * 16);
+            grad_arrive<3>();
+            {  // scale exp(g) dO S, -beta exp(g) r S
+                float part[2][8];
+#pragma unroll
+                for (int lh = 0; lh < 2; ++lh) {
+                    float y[8];
+                    tm_ld16(lanes + (lh << 20) + kTmDOS, part[lh]);
+                    tm_ld16(lanes + (lh << 20) + kTmRS, y);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int t = t0 + i / 4 * 8 + i % 2;
+                        part[lh][i] *= sm.tab[TAB_SEGQ * kC + t];
+                        dq[lh][i] += part[lh][i];
+                        dk[lh][i] = fmaf(-sm.tab[TAB_BEGK * kC + t], y[i], dk[lh][i]);
+                    }
+                }
+                put_dots(part, sm.Q, sm.rowq);
+            }
+            failed |= !wait_products(&bar_load, 1);  // (the second copy of the value head's two)
+            {  // <D, S>
+                float d = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 h4 = *reinterpret_cast<const uint4*>(sm.S + (tid + i * kGradThreads) * 16), m4 = *reinterpret_cast<const uint4*>(sm.S + kImage / 2 + (tid + i * kGradThreads) * 16);
+                    const uint32_t a[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w}, b[4] = {x[1][i].x, x[1][i].y, x[1][i].z, x[1][i].w};
+                    const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, m[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        d = fmaf(bf16_lo(a[e]) - bf16_lo(b[e]), bf16_lo(h[e]) - bf16_lo(m[e]), d);
+                        d = fmaf(bf16_hi(a[e]) - bf16_hi(b[e]), bf16_hi(h[e]) - bf16_hi(m[e]), d);
+                    }
+                }
+                for (int o = 16; o > 0; o /= 2) d += __shfl_xor_sync(0xffffffffu, d, o);
+                if (l.g == 0 && l.c == 0) sm.ds[warp] = d;
+            }
+            grad_arrive<4>();
+            failed |= !wait_products(&bar_out, turn);
+            failed |= !wait_products(&bar_d, turn);
+            tc_fence_after_sync();
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float a[8], b[8], y[8];
+                tm_ld16(lanes + (lh << 20) + kTmDQ, a);
+                tm_ld16(lanes + (lh << 20) + kTmDK, b);
+                tm_ld16(lanes + (lh << 20) + kTmUD, y);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dq[lh][i] += a[i];
+                    dk[lh][i] += fmaf(sm.tab[TAB_ECK * kC + t0 + i / 4 * 8 + i % 2], y[i], b[i]);
+                }
+            }
+            tc_fence_before_sync();
+            __syncthreads();
+        }
+        // through the norm of the rows: x - ||row||^-2 <row, x> row; turned back through shared memory
+        if (p.l2norm) {
+            put_dots(dq, sm.Q, sm.rowq);
+            put_dots(dk, sm.K, sm.rown);
+        }
         __syncthreads();
-    };
-    finish(dq, sm.Q, sm.tab + TAB_RQ * kC, p.dQ);
-    finish(dk, sm.K, sm.tab + TAB_RK * kC, p.dK);
+        __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(sm.S);
+        const auto finish = [&](const float (&x)[2][8], const uint8_t* tile, const float* inv, const float (*dots)[kC], __nv_bfloat16* to) {
+            float c[4] = {};
+            if (p.l2norm) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int t = t0 + e / 2 * 8 + e % 2;
+                    c[e] = inv[t] * inv[t] * ((dots[0][t] + dots[1][t]) + (dots[2][t] + dots[3][t]));
+                }
+            }
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                uint32_t w[4];
+                turned_swizzled(tile, quarter * 16, quad * 32 + lh * 16, w);
+#pragma unroll
+                for (int i = 0; i < 8; i += 2)
+                    w[i / 2] = pack_bf16x2(fmaf(-c[i / 4 * 2], bf16_lo(w[i / 2]), x[lh][i]), fmaf(-c[i / 4 * 2 + 1], bf16_hi(w[i / 2]), x[lh][i + 1]));
+                const int lane = tid % 32;
+                const uint32_t at = smem_u32(to + (quarter * 16 + (lane & 7) + (lane >> 4) * 8) * kLdX + quad * 32 + lh * 16 + ((lane >> 3) & 1) * 8);
+                asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+            }
+        };
+        finish(dq, sm.Q, sm.tab + TAB_RQ * kC, sm.rowq, out);
+        finish(dk, sm.K, sm.tab + TAB_RK * kC, sm.rown, out + kC * kLdX);
+        __syncthreads();
+        const long long at = p.qk.at(s, first, hk);
+        for (int i = tid; i < kC * kD / 8; i += kGradThreads) {
+            const int row = i / 16, col = i % 16 * 8;
+            if (row < rows) {
+                *reinterpret_cast<uint4*>(p.dQ + at + row * p.qk.token + col) = *reinterpret_cast<const uint4*>(out + row * kLdX + col);
+                *reinterpret_cast<uint4*>(p.dK + at + row * p.qk.token + col) = *reinterpret_cast<const uint4*>(out + (kC + row) * kLdX + col);
+            }
+        }
+    }
+    if (failed) *p.status = GDN_ERR_TIMEOUT;
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tm, kTmColumns);
 }
 
 template <typename Smem>
-bool launch(void (*kern)(ParamsB), long long ctas, const ParamsB& p, cudaStream_t stream) {
+bool launch(void (*kern)(ParamsB), long long ctas, unsigned threads, const ParamsB& p, cudaStream_t stream) {
     if (ctas == 0) return true;
-    static_assert(sizeof(Smem) <= 227 * 1024, "");
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Smem)) != cudaSuccess) {
+    static_assert(sizeof(Smem) + 1024 <= 227 * 1024, "");  // (1 KB to start on a multiple of 1 KB)
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Smem) + 1024) != cudaSuccess) {
         cudaGetLastError();
         return false;
     }
-    kern<<<static_cast<unsigned>(ctas), kThreads, sizeof(Smem), stream>>>(p);
+    kern<<<static_cast<unsigned>(ctas), threads, sizeof(Smem) + 1024, stream>>>(p);
     if (cudaGetLastError() != cudaSuccess) return false;
     count_launch();
     return true;
@@ -971,6 +1429,8 @@ int launch_layer_backward(const ProblemB& q, cudaStream_t stream) {
     p.dQ = static_cast<__nv_bfloat16*>(q.dQ), p.dK = static_cast<__nv_bfloat16*>(q.dK), p.dV = static_cast<__nv_bfloat16*>(q.dV);
     p.dbeta = q.dbeta, p.dg = q.dg, p.dS_in = q.dS_in, p.ws = static_cast<float*>(q.workspace), p.cu = q.cu_seqlens;
     p.n_seq = q.n_seq, p.T = q.T, p.H_k = q.H_k, p.H_v = q.H_v, p.group = q.H_v / q.H_k, p.chunks = (q.T + kC - 1) / kC;
+    p.status = device_status_word();
+    if (p.status == nullptr) return GDN_ERR_LAUNCH;
     p.scale = q.scale, p.l2norm = (q.flags & GDN_FLAG_K_L2NORM) != 0;
     const bool token_major = (q.flags & GDN_FLAG_LAYOUT_BTHD) != 0, packed = q.cu_seqlens != nullptr;
     const auto strides = [&](long long H, long long d) {
@@ -980,10 +1440,12 @@ int launch_layer_backward(const ProblemB& q, cudaStream_t stream) {
     };
     p.qk = strides(q.H_k, kD), p.v = strides(q.H_v, kD), p.gate = strides(q.H_v, 1);
     const long long places = packed ? chunk_places(q.n_seq, q.T) : static_cast<long long>(q.n_seq) * p.chunks;
-    const long long chains = static_cast<long long>(q.n_seq) * q.H_v * kSlices;
+    const long long chains = static_cast<long long>(q.n_seq) * q.H_v;
     if (places * q.H_k >= (1LL << 31) || chains >= (1LL << 31)) return GDN_ERR_UNSUPPORTED;
-    const bool ok = launch<SmemSystem>(chunk_system_kernel, places * q.H_k, p, stream) && launch<SmemF>(chunk_states_kernel, chains, p, stream) &&
-                    launch<SmemB>(chunk_state_grads_kernel, chains, p, stream) && launch<SmemC>(chunk_grads_kernel, places * q.H_k, p, stream);
+    const bool ok = launch<SmemSystem>(chunk_system_kernel, places * q.H_k, kThreads, p, stream) &&
+                    launch<SmemF>(chunk_states_kernel, chains, kChainThreads, p, stream) &&
+                    launch<SmemB>(chunk_state_grads_kernel, chains, kChainThreads, p, stream) &&
+                    launch<SmemC>(chunk_grads_kernel, places * q.H_k, kGradThreads + 32, p, stream);
     return ok ? GDN_OK : GDN_ERR_LAUNCH;
 }
 
