@@ -404,6 +404,10 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
                  : "memory");
 }
+// brings them into L2
+__device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(src)), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)), "r"(smem_u32(src)), "r"(bytes) : "memory");
 }
@@ -422,14 +426,14 @@ __device__ __forceinline__ void publish() {
     tmem_wait_st();
     tc_fence_before_sync();
 }
-// hand-offs: `from` threads arrive and go on, a warp waits. Each is passed once a chunk, and a barrier of the whole CTA lies between two chunks.
-template <int ID>
+// hand-offs: the computing warps arrive and go on, N threads wait. Each is passed once a chunk, and a barrier of the whole CTA lies between two chunks.
+template <int ID, int N = 32>
 __device__ __forceinline__ void arrive() {
-    asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kThreads + 32) : "memory");
+    asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kThreads + N) : "memory");
 }
-template <int ID>
+template <int ID, int N = 32>
 __device__ __forceinline__ void await() {
-    asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kThreads + 32) : "memory");
+    asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kThreads + N) : "memory");
 }
 
 // Products of the chains, each issued by one thread. A [128 lanes x K] in three pieces of K / 2 columns at `a`; the small ones first.
@@ -457,7 +461,13 @@ __device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t x,
                 mma_f16_ts(d + half * 64, a + i * 32 + k * 8, b + (half * kTile + k * 2048) / 16, kIdescCols | (i == 1 ? kNegA : 0u),
                            more || i < kPieces - 1 || k > 0);
 }
-// d = A M^T (COLS: A M), both in three pieces, M 64 x 64 in three tiles: the six products of pieces that fp32 can hold
+// d = A M^T (COLS: A M), both in three pieces, M 64 x 64 and lower triangular in three tiles: the six products of pieces that fp32 can hold, each
+// 16 of the sum at a time and as many columns as those have a part in (from 16 k on; COLS: up to 16 k + 15), the one with all 64 first
+template <bool COLS>
+__device__ __forceinline__ void product_block(uint32_t d, uint32_t a, uint64_t b, int k, bool minus, bool more) {
+    const uint32_t idesc = instr_desc(128, COLS ? 16 * k + 16 : 64 - 16 * k, 1, 1, 0, COLS, 1) | (minus ? kNegA : 0u);
+    mma_f16_ts(COLS ? d : d + 16 * k, a + k * 8, b + (COLS ? k * 2048 : k * (2048 + 32)) / 16, idesc, more);
+}
 template <bool COLS>
 __device__ __forceinline__ void product_system(uint32_t d, uint32_t a, uint32_t tiles) {
     const uint64_t b = COLS ? desc_cols(tiles) : desc_rows(tiles);
@@ -468,12 +478,19 @@ __device__ __forceinline__ void product_system(uint32_t d, uint32_t a, uint32_t 
         for (int i = sum; i >= 0; --i) {
             const int j = sum - i;  // the pieces of A and M; one middle piece: negated
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                mma_f16_ts(d, a + i * 32 + k * 8, b + (j * kTile + k * (COLS ? 2048 : 32)) / 16,
-                           (COLS ? kIdescCols : kIdescRows) | ((i == 1) != (j == 1) ? kNegA : 0u), more);
+            for (int q = 0; q < 4; ++q) {
+                product_block<COLS>(d, a + i * 32, b + j * kTile / 16, COLS ? 3 - q : q, (i == 1) != (j == 1), more);
                 more = true;
             }
         }
+}
+// d = A P, A [128 x 64 tokens] bf16, P lower triangular in three tiles
+__device__ __forceinline__ void product_pairs(uint32_t d, uint32_t a, uint32_t tiles) {
+    const uint64_t b = desc_cols(tiles);
+#pragma unroll
+    for (int i = kPieces - 1; i >= 0; --i)
+#pragma unroll
+        for (int k = 3; k >= 0; --k) product_block<true>(d, a, b + i * kTile / 16, k, i == 1, i < kPieces - 1 || k < 3);
 }
 
 // a value for each of a thread's 8 x 2 rows and columns: `f(row, column, i)` gets the place of x[i], x[i + 1] (neighbouring columns)
@@ -484,7 +501,8 @@ __device__ __forceinline__ void for_pairs(const F& f) {
     for (int i = 0; i < N; i += 2) f(l.g + ((i >> 1) & 1) * 8, (i >> 2) * 8 + 2 * l.c, i);
 }
 
-constexpr int kChainThreads = kThreads + 64;  // eight warps that compute, one that issues the products, one that loads and stores tiles
+constexpr int kLoaders = 96;
+constexpr int kChainThreads = kThreads + 32 + kLoaders;  // eight warps that compute, one that issues the products, three that load and store tiles
 constexpr int kImage = 2 * 2 * 2 * kTile;     // bytes of a state's tiles: two pieces of two tiles of 128 rows
 // Byte of element (row, col) of a state in its image
 __device__ __forceinline__ int image_at(int piece, int row, int col) { return (piece * 2 + col / 64) * 2 * kTile + swizzled(row, col % 64); }
@@ -592,7 +610,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             __syncwarp();
         }
     } else if (warp > kThreads / 32) {  // ---- the tiles
-        const int me = threadIdx.x % 32;
+        const int me = threadIdx.x - kThreads - 32;
         const auto load = [&](int c) {
             if (c < n) {
                 StageF& st = sm.stage[c % 2];
@@ -602,8 +620,8 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
                     bulk_load(st.T, ws + kWsT, sizeof(st.T), ch.full);
                     bulk_load(st.tab, ws + kWsTab, sizeof(st.tab), ch.full);
                 }
-                copy_tile<32>(st.K, p.K + p.qk.at(s, seq.first + c * kC, hk), p.qk.token, seq.len - c * kC, me);
-                copy_plain<32>(st.V, p.V + p.v.at(s, seq.first + c * kC, h), p.v.token, seq.len - c * kC, me);
+                copy_tile<kLoaders>(st.K, p.K + p.qk.at(s, seq.first + c * kC, hk), p.qk.token, seq.len - c * kC, me);
+                copy_plain<kLoaders>(st.V, p.V + p.v.at(s, seq.first + c * kC, h), p.v.token, seq.len - c * kC, me);
                 cp_commit();
             }
         };
@@ -615,7 +633,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             ch.failed |= !wait_products(ch.full, c & 1);
             if (__syncthreads_or(ch.failed)) break;
             load(c + 1);
-            await<3>();
+            await<3, kLoaders>();
             if (me == 0) {
                 bulk_store(chunk_ws(p, seq.slot + c, h) + kWsS, sm.image, kImage);
                 tma_store_commit();
@@ -643,7 +661,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             if (__syncthreads_or(ch.failed)) break;
             put_image(sm.image, S, row0, half);
             fence_proxy_async_smem();
-            arrive<3>();
+            arrive<3, kLoaders>();
             uint32_t v[2][8];
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
@@ -748,12 +766,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             await<1>();
             tc_fence_after_sync();
             if (elect_one()) {  // dO^T P
-                const uint64_t b = desc_cols(smem_u32(sm.P));
-#pragma unroll
-                for (int i = kPieces - 1; i >= 0; --i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        mma_f16_ts(ch.tm + kTmX, ch.tm + kTmO + k * 8, b + (i * kTile + k * 2048) / 16, kIdescCols | (i == 1 ? kNegA : 0u), i < kPieces - 1 || k > 0);
+                product_pairs(ch.tm + kTmX, ch.tm + kTmO, smem_u32(sm.P));
                 mma_commit(ch.done);
             }
             __syncwarp();
@@ -777,15 +790,15 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             __syncwarp();
         }
     } else if (warp > kThreads / 32) {  // ---- the tiles
-        const int me = threadIdx.x % 32;
+        const int me = threadIdx.x - kThreads - 32;
         uint32_t turn = 0;
         const auto load = [&](int c) {
             if (c >= 0) {
                 StageB& st = sm.stage[c % 2];
                 const int t = seq.first + c * kC, rows = seq.len - c * kC;
-                copy_tile<32>(st.K, p.K + p.qk.at(s, t, hk), p.qk.token, rows, me);
-                copy_tile<32>(st.Q, p.Q + p.qk.at(s, t, hk), p.qk.token, rows, me);
-                copy_plain<32>(st.dO, p.dO + p.v.at(s, t, h), p.v.token, rows, me);
+                copy_tile<kLoaders>(st.K, p.K + p.qk.at(s, t, hk), p.qk.token, rows, me);
+                copy_tile<kLoaders>(st.Q, p.Q + p.qk.at(s, t, hk), p.qk.token, rows, me);
+                copy_plain<kLoaders>(st.dO, p.dO + p.v.at(s, t, h), p.v.token, rows, me);
                 cp_commit();
             }
         };
@@ -808,13 +821,13 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             turn ^= 1;
             if (__syncthreads_or(ch.failed)) break;
             load(c - 1);
-            await<5>();
+            await<5, kLoaders>();
             if (me == 0) {
                 bulk_store(chunk_ws(p, seq.slot + c, h) + kWsDS, sm.image, kImage);
                 tma_store_commit();
             }
             __syncwarp();
-            await<6>();  // T and P are used up
+            await<6, kLoaders>();  // T and P are used up
             load_system(c - 1);
         }
         tma_store_wait_all<0>();
@@ -854,7 +867,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
                 });
             put_image(sm.image, D, row0, half);
             fence_proxy_async_smem();
-            arrive<5>();
+            arrive<5, kLoaders>();
             ch.wait();
             float dots[kDots][8] = {};  // of this thread's eight tokens: 8 (i / 4) + 2 c + e at [i / 4 * 2 + e]
 #pragma unroll
@@ -896,7 +909,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             publish();
             arrive<3>();
             ch.wait();  // (for r; what was issued behind it may still run)
-            arrive<6>();
+            arrive<6, kLoaders>();
             float r[2][16];
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
@@ -1077,6 +1090,13 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 __syncwarp();
             };
             load(ws + kWsS);
+            if (it == 0 && elect_one()) {  // what the CTA that follows on some SM will ask for: on its way into L2
+                int s1, first1, rows1;
+                const int next = blockIdx.x + kSMs;
+                if (next < static_cast<int>(gridDim.x) && chunk_of(p, next / p.H_k, s1, first1, rows1))
+                    bulk_prefetch(chunk_ws(p, next / p.H_k, next % p.H_k * heads) + kWsS, (kWsTab - kWsS) * 4);
+            }
+            __syncwarp();
             grad_await<1>();  // K, Q, dO, u, r are there
             tc_fence_after_sync();
             if (elect_one()) {
