@@ -408,6 +408,7 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 __device__ __forceinline__ void bulk_prefetch(const void* src, uint32_t bytes) {
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(src)), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void prefetch_l2(const void* line) { asm volatile("prefetch.global.L2 [%0];" ::"l"(line) : "memory"); }
 __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)), "r"(smem_u32(src)), "r"(bytes) : "memory");
 }
@@ -989,7 +990,7 @@ struct SmemC {
     uint8_t S[kImage];                                     // the state, then its gradient; at the end dQ and dK on their way out
     uint8_t u[kPieces][2 * kTile], r[kPieces][2 * kTile];  // [v][token]; in the place of the third pieces, p and m: two pieces each
     float tab[kTabs * kC];
-    float rowq[4][kC], rown[4][kC], rowb[4][kC], coln[4][kC], rv[2][kC];
+    float rowq[4][kC], rown[4][kC], rowb[4][kC], coln[4][kC], rv[2][kC], norm[2][4][kC];
     float ds[kGradThreads / 32];
 };
 static_assert(2 * kC * kLdX * 2 <= kImage, "");
@@ -1078,6 +1079,22 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
         const auto tile_u = [&](int i) { return smem_u32(sm.u[i]); };
         const auto tile_r = [&](int i) { return smem_u32(sm.r[i]); };
         const auto state = [&](int i) { return smem_desc(S + i * (kImage / 2), 2 * kTile, 1024, SWZ_128B); };
+        // what the CTA that is next on some SM will ask for comes into L2 while this one has what it needs: the HBM would idle here,
+        // and be what everybody waits for there
+        const auto prefetch = [&](int block) {
+            int s1, first1, rows1;
+            if (block >= static_cast<int>(gridDim.x) || !chunk_of(p, block / p.H_k, s1, first1, rows1)) return;
+            const int hk1 = block % p.H_k, lane = tid % 32;
+            if (elect_one()) bulk_prefetch(chunk_ws(p, block / p.H_k, hk1 * heads) + kWsS, (kWsTab - kWsS) * 4);
+            __syncwarp();
+            for (int i = lane; i < 2 * rows1; i += 32) {
+                const long long q = p.qk.at(s1, first1 + i / 2, hk1) + i % 2 * 64, v = p.v.at(s1, first1 + i / 2, hk1 * heads) + i % 2 * 64;
+                prefetch_l2(p.K + q);
+                prefetch_l2(p.Q + q);
+                prefetch_l2(p.dO + v);
+                prefetch_l2(p.V + v);
+            }
+        };
         uint32_t loads = 0;
         for (int it = 0; it < heads; ++it) {
             const int hv = hk * heads + it;
@@ -1090,15 +1107,19 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 __syncwarp();
             };
             load(ws + kWsS);
-            if (it == 0 && elect_one()) {  // what the CTA that follows on some SM will ask for: on its way into L2
-                int s1, first1, rows1;
-                const int next = blockIdx.x + kSMs;
-                if (next < static_cast<int>(gridDim.x) && chunk_of(p, next / p.H_k, s1, first1, rows1))
-                    bulk_prefetch(chunk_ws(p, next / p.H_k, next % p.H_k * heads) + kWsS, (kWsTab - kWsS) * 4);
-            }
-            __syncwarp();
             grad_await<1>();  // K, Q, dO, u, r are there
             tc_fence_after_sync();
+            failed |= !wait_products(&bar_load, loads++ & 1);
+            if (it == 0) prefetch(blockIdx.x + kSMs);
+            if (elect_one()) {
+                product<8>(tm + kTmDOS, state(1), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, true), false);
+                product<8>(tm + kTmDOS, state(0), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, false), true);
+                product<8>(tm + kTmRS, state(1), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, true), false);
+                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(1)), kDown, grad_idesc(128, true, true, true), true);
+                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, false), true);
+                mma_commit(&bar_s);
+            }
+            __syncwarp();
             if (elect_one()) {
 #pragma unroll
                 for (int i = kPieces - 1; i >= 0; --i)
@@ -1114,16 +1135,8 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 mma_commit(&bar_pair);
             }
             __syncwarp();
-            failed |= !wait_products(&bar_load, loads++ & 1);
-            if (elect_one()) {
-                product<8>(tm + kTmDOS, state(1), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, true), false);
-                product<8>(tm + kTmDOS, state(0), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, false), true);
-                product<8>(tm + kTmRS, state(1), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, true), false);
-                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(1)), kDown, grad_idesc(128, true, true, true), true);
-                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, false), true);
-                mma_commit(&bar_s);
-            }
-            __syncwarp();
+            grad_await<3>();  // the state is used up
+            load(ws + kWsDS);
             grad_await<2>();  // p, m
             tc_fence_after_sync();
             if (elect_one()) {
@@ -1139,8 +1152,6 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 mma_commit(&bar_out);
             }
             __syncwarp();
-            grad_await<3>();  // the state is used up
-            load(ws + kWsDS);
             failed |= !wait_products(&bar_load, loads++ & 1);
             if (elect_one()) {
                 product<8>(tm + kTmUD, state(1), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, true), false);
@@ -1176,10 +1187,8 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             }
             if (2 * lane < rows) p.dg[p.gate.at(s, first + 2 * lane, hv)] = sum;
             if (2 * lane + 1 < rows) p.dg[p.gate.at(s, first + 2 * lane + 1, hv)] = sum - d[0];
-            __syncthreads();
+            if (it + 1 < heads) __syncthreads();
         }
-        __syncthreads();
-        __syncthreads();
     } else {
         const int quad = warp % 4, quarter = warp / 4;  // 32 key features (16 tokens of p, m), 16 tokens
         const uint32_t lanes = tm + (static_cast<uint32_t>(quad * 32) << 16) + quarter * 16;
@@ -1210,6 +1219,12 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             copy_tile<kGradThreads>(sm.dO, p.dO + p.v.at(s, first, hv), p.v.token, rows, tid);
             for (int i = tid * 4; i < kTabs * kC; i += kGradThreads * 4) cp16(sm.tab + i, ws + kWsTab + i, true);
             cp_commit();
+            // V for <r, v>, eight tokens a warp and half of the features (see below): asked for here
+            uint32_t v[8];
+            const int row_v = warp % 8 * 8 + l.g;
+            const long long at_v = p.v.at(s, first + row_v, hv) + warp / 8 * 64 + 2 * l.c;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = row_v < rows ? *reinterpret_cast<const uint32_t*>(p.V + at_v + i * 8) : 0u;
             {  // u and r in pieces
                 float4 x[2][4];
 #pragma unroll
@@ -1235,29 +1250,32 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             grad_arrive<1>();
             grad_sync();
             {  // dV = beta r, turned back, and <r, v>
-                const int t = warp % 8 * 8, v0 = warp / 8 * 64, row = t + l.g;
-                const float b = sm.tab[TAB_BETA * kC + row];
-                const long long at = p.v.at(s, first + row, hv) + v0 + 2 * l.c;
+                const float b = sm.tab[TAB_BETA * kC + row_v];
                 float rv = 0.f;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t w[kPieces][4];
-                    const int v = v0 + i * 32 + tid % 32;
 #pragma unroll
-                    for (int q = 0; q < kPieces; ++q) ldmatrix_turned(smem_u32(sm.r[q] + swizzled(v, t)), w[q]);
-                    if (row < rows) {
+                    for (int q = 0; q < kPieces; ++q) ldmatrix_turned(smem_u32(sm.r[q] + swizzled(warp / 8 * 64 + i * 32 + tid % 32, warp % 8 * 8)), w[q]);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float x = (bf16_lo(w[0][k]) - bf16_lo(w[1][k])) + bf16_lo(w[2][k]), y = (bf16_hi(w[0][k]) - bf16_hi(w[1][k])) + bf16_hi(w[2][k]);
-                            const uint32_t vv = *reinterpret_cast<const uint32_t*>(p.V + at + i * 32 + k * 8);
-                            rv = fmaf(x, bf16_lo(vv), fmaf(y, bf16_hi(vv), rv));
-                            *reinterpret_cast<uint32_t*>(p.dV + at + i * 32 + k * 8) = pack_bf16x2(b * x, b * y);
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        const float x = (bf16_lo(w[0][k]) - bf16_lo(w[1][k])) + bf16_lo(w[2][k]), y = (bf16_hi(w[0][k]) - bf16_hi(w[1][k])) + bf16_hi(w[2][k]);
+                        rv = fmaf(x, bf16_lo(v[i * 4 + k]), fmaf(y, bf16_hi(v[i * 4 + k]), rv));
+                        if (row_v < rows) *reinterpret_cast<uint32_t*>(p.dV + at_v + i * 32 + k * 8) = pack_bf16x2(b * x, b * y);
                     }
                 }
                 rv = quad_sum(rv);
-                if (l.c == 0) sm.rv[warp / 8][row] = rv;
+                if (l.c == 0) sm.rv[warp / 8][row_v] = rv;
             }
+            failed |= !wait_products(&bar_load, 0);
+            failed |= !wait_products(&bar_s, turn);
+            tc_fence_after_sync();
+            uint4 x[2][4];
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[q][i] = *reinterpret_cast<const uint4*>(sm.S + q * (kImage / 2) + (tid + i * kGradThreads) * 16);
+            grad_arrive<3>();
             grad_sync();  // the third pieces make room
             failed |= !wait_products(&bar_pair, turn);
             tc_fence_after_sync();
@@ -1309,15 +1327,6 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 const float sum = token_sum(coln, l);
                 if ((l.g & 1) == 0) sm.coln[quad][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
             }
-            failed |= !wait_products(&bar_load, 0);
-            failed |= !wait_products(&bar_s, turn);
-            tc_fence_after_sync();
-            uint4 x[2][4];
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[q][i] = *reinterpret_cast<const uint4*>(sm.S + q * (kImage / 2) + (tid + i * kGradThreads) * 16);
-            grad_arrive<3>();
             {  // scale exp(g) dO S, -beta exp(g) r S
                 float part[2][8];
 #pragma unroll
@@ -1371,14 +1380,14 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 }
             }
             tc_fence_before_sync();
-            __syncthreads();
+            if (it + 1 < heads) __syncthreads();
         }
         // through the norm of the rows: x - ||row||^-2 <row, x> row; turned back through shared memory
         if (p.l2norm) {
-            put_dots(dq, sm.Q, sm.rowq);
-            put_dots(dk, sm.K, sm.rown);
+            put_dots(dq, sm.Q, sm.norm[0]);
+            put_dots(dk, sm.K, sm.norm[1]);
         }
-        __syncthreads();
+        grad_sync();
         __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(sm.S);
         const auto finish = [&](const float (&x)[2][8], const uint8_t* tile, const float* inv, const float (*dots)[kC], __nv_bfloat16* to) {
             float c[4] = {};
@@ -1401,9 +1410,9 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
             }
         };
-        finish(dq, sm.Q, sm.tab + TAB_RQ * kC, sm.rowq, out);
-        finish(dk, sm.K, sm.tab + TAB_RK * kC, sm.rown, out + kC * kLdX);
-        __syncthreads();
+        finish(dq, sm.Q, sm.tab + TAB_RQ * kC, sm.norm[0], out);
+        finish(dk, sm.K, sm.tab + TAB_RK * kC, sm.norm[1], out + kC * kLdX);
+        grad_sync();
         const long long at = p.qk.at(s, first, hk);
         for (int i = tid; i < kC * kD / 8; i += kGradThreads) {
             const int row = i / 16, col = i % 16 * 8;
