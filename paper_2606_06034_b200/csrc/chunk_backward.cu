@@ -62,6 +62,7 @@ struct ParamsB {
     int* status;
     const int* cu;  // packed sequences: their boundaries; null: n_seq sequences of T tokens
     int n_seq, T, H_k, H_v, group, chunks;  // chunks: of a dense sequence
+    long long units;                        // places of chunks in the workspace times key heads
     Strides qk, v, gate;
     float scale;
     bool l2norm;
@@ -987,13 +988,18 @@ constexpr int kGradThreads = 512;  // 16 warps, and one that issues the products
 
 struct SmemC {
     uint8_t K[2 * kTile], Q[2 * kTile], dO[2 * kTile];
-    uint8_t S[kImage];                                     // the state, then its gradient; at the end dQ and dK on their way out
-    uint8_t u[kPieces][2 * kTile], r[kPieces][2 * kTile];  // [v][token]; in the place of the third pieces, p and m: two pieces each
+    uint8_t S[kImage];                                     // the state, then its gradient
+    // [v][token] in pieces. Before that u and r as they come, in the first 64 KB; later p and m in the place of the third pieces, two
+    // pieces each; at the end dQ and dK on their way out, in the last 32 KB
+    uint8_t u[kPieces][2 * kTile], r[kPieces][2 * kTile];
     float tab[kTabs * kC];
     float rowq[4][kC], rown[4][kC], rowb[4][kC], coln[4][kC], rv[2][kC], norm[2][4][kC];
     float ds[kGradThreads / 32];
 };
-static_assert(2 * kC * kLdX * 2 <= kImage, "");
+constexpr int kRaw = kC * kD * 4;  // bytes of u or r
+struct Unit {  // what a CTA takes next: a chunk of a key head
+    int ok, slot, hk, s, first, rows;
+};
 
 __device__ __forceinline__ void tm_ld16(uint32_t taddr, float (&x)[8]) {  // 16 lanes x 16 columns
     uint32_t r[8];
@@ -1054,13 +1060,24 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
     SmemC& sm = *reinterpret_cast<SmemC*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
     __shared__ uint64_t bar_pair, bar_s, bar_out, bar_d, bar_load;
     __shared__ uint32_t base;
-    const int hk = blockIdx.x % p.H_k, slot = blockIdx.x / p.H_k;
-    int s, first, rows;
-    if (!chunk_of(p, slot, s, first, rows)) return;
+    __shared__ Unit units[2];
     const int tid = threadIdx.x, warp = tid / 32;
     const Lane l;
     bool failed = false;
+    // the unit at or after place `at` of this CTA's (every gridDim.x-th); places that hold no chunk are passed over
+    const auto find_unit = [&](long long at) {
+        Unit x{0, 0, 0, 0, 0, 0};
+        for (; at < p.units; at += gridDim.x) {
+            x.slot = static_cast<int>(at / p.H_k), x.hk = static_cast<int>(at % p.H_k);
+            if (chunk_of(p, x.slot, x.s, x.first, x.rows)) {
+                x.ok = 1;
+                break;
+            }
+        }
+        return x;
+    };
     if (tid == 0) {
+        units[0] = find_unit(blockIdx.x);
         for (uint64_t* b : {&bar_pair, &bar_s, &bar_out, &bar_d, &bar_load}) mbar_init(b, 1);
         mbar_fence_init();
     }
@@ -1079,38 +1096,45 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
         const auto tile_u = [&](int i) { return smem_u32(sm.u[i]); };
         const auto tile_r = [&](int i) { return smem_u32(sm.r[i]); };
         const auto state = [&](int i) { return smem_desc(S + i * (kImage / 2), 2 * kTile, 1024, SWZ_128B); };
-        // what the CTA that is next on some SM will ask for comes into L2 while this one has what it needs: the HBM would idle here,
-        // and be what everybody waits for there
-        const auto prefetch = [&](int block) {
-            int s1, first1, rows1;
-            if (block >= static_cast<int>(gridDim.x) || !chunk_of(p, block / p.H_k, s1, first1, rows1)) return;
-            const int hk1 = block % p.H_k, lane = tid % 32;
-            if (elect_one()) bulk_prefetch(chunk_ws(p, block / p.H_k, hk1 * heads) + kWsS, (kWsTab - kWsS) * 4);
+        // What is asked for next comes into L2 while the products of the present head run: the HBM would idle then, and be what everybody
+        // waits for later
+        const auto prefetch = [&](const Unit& x, int hv, bool keys) {
+            if (!x.ok) return;
+            if (elect_one()) bulk_prefetch(chunk_ws(p, x.slot, hv) + kWsS, (kWsTab - kWsS) * 4);
             __syncwarp();
-            for (int i = lane; i < 2 * rows1; i += 32) {
-                const long long q = p.qk.at(s1, first1 + i / 2, hk1) + i % 2 * 64, v = p.v.at(s1, first1 + i / 2, hk1 * heads) + i % 2 * 64;
-                prefetch_l2(p.K + q);
-                prefetch_l2(p.Q + q);
+            for (int i = tid % 32; i < 2 * x.rows; i += 32) {
+                const long long q = p.qk.at(x.s, x.first + i / 2, x.hk) + i % 2 * 64, v = p.v.at(x.s, x.first + i / 2, hv) + i % 2 * 64;
+                if (keys) prefetch_l2(p.K + q), prefetch_l2(p.Q + q);
                 prefetch_l2(p.dO + v);
                 prefetch_l2(p.V + v);
             }
         };
-        uint32_t loads = 0;
-        for (int it = 0; it < heads; ++it) {
-            const int hv = hk * heads + it;
-            float* const ws = chunk_ws(p, slot, hv);
-            const auto load = [&](const float* from) {
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(&bar_load, kImage);
-                    bulk_load(sm.S, from, kImage, &bar_load);
-                }
+        const auto load = [&](const float* ws) {  // S, u and r of a value head
+            if (elect_one()) {
+                mbar_arrive_expect_tx(&bar_load, kImage + 2 * kRaw);
+                bulk_load(sm.u, ws + kWsU, 2 * kRaw, &bar_load);
+                bulk_load(sm.S, ws + kWsS, kImage, &bar_load);
+            }
+            __syncwarp();
+        };
+        uint32_t phase = 0;
+        Unit now = units[0];
+        if (now.ok) load(chunk_ws(p, now.slot, now.hk * heads));
+        long long place = blockIdx.x;
+        for (int n = 0, it = 0; now.ok;) {
+            const int hv = now.hk * heads + it, s = now.s, first = now.first, rows = now.rows;
+            float* const ws = chunk_ws(p, now.slot, hv);
+            const bool last = it + 1 == heads;
+            Unit next = now;
+            if (last) {
+                place = static_cast<long long>(now.slot) * p.H_k + now.hk + gridDim.x;
+                next = find_unit(place);
+                if (elect_one()) units[(n + 1) & 1] = next;
                 __syncwarp();
-            };
-            load(ws + kWsS);
+            }
+            const int next_hv = last ? next.hk * heads : hv + 1;
             grad_await<1>();  // K, Q, dO, u, r are there
             tc_fence_after_sync();
-            failed |= !wait_products(&bar_load, loads++ & 1);
-            if (it == 0) prefetch(blockIdx.x + kSMs);
             if (elect_one()) {
                 product<8>(tm + kTmDOS, state(1), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, true), false);
                 product<8>(tm + kTmDOS, state(0), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, false), true);
@@ -1135,8 +1159,13 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 mma_commit(&bar_pair);
             }
             __syncwarp();
+            prefetch(next, next_hv, last);
             grad_await<3>();  // the state is used up
-            load(ws + kWsDS);
+            if (elect_one()) {
+                mbar_arrive_expect_tx(&bar_load, kImage);
+                bulk_load(sm.S, ws + kWsDS, kImage, &bar_load);
+            }
+            __syncwarp();
             grad_await<2>();  // p, m
             tc_fence_after_sync();
             if (elect_one()) {
@@ -1152,7 +1181,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 mma_commit(&bar_out);
             }
             __syncwarp();
-            failed |= !wait_products(&bar_load, loads++ & 1);
+            failed |= !wait_products(&bar_load, 1);
             if (elect_one()) {
                 product<8>(tm + kTmUD, state(1), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, true), false);
                 product<8>(tm + kTmUD, state(0), kDown, desc_cols(tile_u(1)), kDown, grad_idesc(128, true, true, true), true);
@@ -1160,7 +1189,11 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 mma_commit(&bar_d);
             }
             __syncwarp();
-            grad_await<4>();  // every part of dbeta and dg. Lane i has tokens 2i, 2i + 1
+            grad_await<4>();  // every part of dbeta and dg; the state's gradient is read
+            failed |= !wait_products(&bar_d, phase);
+            phase ^= 1;
+            if (next.ok) load(chunk_ws(p, next.slot, next_hv));
+            // lane i has tokens 2i, 2i + 1
             const int lane = tid % 32;
             float d[2], ends = 0.f;
 #pragma unroll
@@ -1187,15 +1220,15 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             }
             if (2 * lane < rows) p.dg[p.gate.at(s, first + 2 * lane, hv)] = sum;
             if (2 * lane + 1 < rows) p.dg[p.gate.at(s, first + 2 * lane + 1, hv)] = sum - d[0];
-            if (it + 1 < heads) __syncthreads();
+            __syncthreads();
+            now = next;
+            it = last ? 0 : it + 1;
+            n += last;
         }
     } else {
         const int quad = warp % 4, quarter = warp / 4;  // 32 key features (16 tokens of p, m), 16 tokens
         const uint32_t lanes = tm + (static_cast<uint32_t>(quad * 32) << 16) + quarter * 16;
         const int t0 = quarter * 16 + 2 * l.c;  // this thread's tokens: t0, t0 + 1, t0 + 8, t0 + 9
-        float dq[2][8] = {}, dk[2][8] = {};     // [16 lanes][see for_pairs], times 1 / ||q||, 1 / ||k||
-        copy_tile<kGradThreads>(sm.K, p.K + p.qk.at(s, first, hk), p.qk.token, rows, tid);
-        copy_tile<kGradThreads>(sm.Q, p.Q + p.qk.at(s, first, hk), p.qk.token, rows, tid);
         // a token's sum over the features of x times K or Q, in four parts
         const auto put_dots = [&](const float (&x)[2][8], const uint8_t* tile, float (*to)[kC]) {
             float d[4] = {};
@@ -1212,26 +1245,36 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             const float sum = token_sum(d, l);
             if ((l.g & 1) == 0) to[quad][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
         };
-        for (int it = 0; it < heads; ++it) {
-            const int hv = hk * heads + it;
-            const uint32_t turn = it & 1;
-            const float* const ws = chunk_ws(p, slot, hv);
-            copy_tile<kGradThreads>(sm.dO, p.dO + p.v.at(s, first, hv), p.v.token, rows, tid);
-            for (int i = tid * 4; i < kTabs * kC; i += kGradThreads * 4) cp16(sm.tab + i, ws + kWsTab + i, true);
+        // the tiles and tables of a value head; V for <r, v>, eight tokens a warp and half of the features
+        uint32_t v[8];
+        const int row_v = warp % 8 * 8 + l.g;
+        const auto ask = [&](const Unit& x, int hv, bool keys) {
+            if (keys) {
+                copy_tile<kGradThreads>(sm.K, p.K + p.qk.at(x.s, x.first, x.hk), p.qk.token, x.rows, tid);
+                copy_tile<kGradThreads>(sm.Q, p.Q + p.qk.at(x.s, x.first, x.hk), p.qk.token, x.rows, tid);
+            }
+            copy_tile<kGradThreads>(sm.dO, p.dO + p.v.at(x.s, x.first, hv), p.v.token, x.rows, tid);
+            if (tid < kTabs * kC / 4) cp16(sm.tab + tid * 4, chunk_ws(p, x.slot, hv) + kWsTab + tid * 4, true);
             cp_commit();
-            // V for <r, v>, eight tokens a warp and half of the features (see below): asked for here
-            uint32_t v[8];
-            const int row_v = warp % 8 * 8 + l.g;
-            const long long at_v = p.v.at(s, first + row_v, hv) + warp / 8 * 64 + 2 * l.c;
+            const long long at = p.v.at(x.s, x.first + row_v, hv) + warp / 8 * 64 + 2 * l.c;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = row_v < rows ? *reinterpret_cast<const uint32_t*>(p.V + at_v + i * 8) : 0u;
+            for (int i = 0; i < 8; ++i) v[i] = row_v < x.rows ? *reinterpret_cast<const uint32_t*>(p.V + at + i * 8) : 0u;
+        };
+        float dq[2][8] = {}, dk[2][8] = {};  // [16 lanes][see for_pairs], times 1 / ||q||, 1 / ||k||
+        Unit now = units[0];
+        if (now.ok) ask(now, now.hk * heads, true);
+        uint32_t turn = 0;
+        for (int n = 0, it = 0; now.ok; turn ^= 1) {
+            const int hv = now.hk * heads + it, s = now.s, first = now.first, rows = now.rows;
+            const bool last = it + 1 == heads;
+            failed |= !wait_products(&bar_load, 0);
             {  // u and r in pieces
                 float4 x[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[0][i] = reinterpret_cast<const float4*>(ws + kWsU)[tid + i * kGradThreads];
-                    x[1][i] = reinterpret_cast<const float4*>(ws + kWsZ)[tid + i * kGradThreads];
-                }
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][i] = reinterpret_cast<const float4*>(&sm.u[0][0] + t * kRaw)[tid + i * kGradThreads];
+                grad_sync();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int at = tid + i * kGradThreads, place = swizzled(at / 16, at % 16 * 4);
@@ -1251,6 +1294,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             grad_sync();
             {  // dV = beta r, turned back, and <r, v>
                 const float b = sm.tab[TAB_BETA * kC + row_v];
+                const long long at_v = p.v.at(s, first + row_v, hv) + warp / 8 * 64 + 2 * l.c;
                 float rv = 0.f;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -1267,7 +1311,6 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 rv = quad_sum(rv);
                 if (l.c == 0) sm.rv[warp / 8][row_v] = rv;
             }
-            failed |= !wait_products(&bar_load, 0);
             failed |= !wait_products(&bar_s, turn);
             tc_fence_after_sync();
             uint4 x[2][4];
@@ -1380,46 +1423,64 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 }
             }
             tc_fence_before_sync();
-            if (it + 1 < heads) __syncthreads();
-        }
-        // through the norm of the rows: x - ||row||^-2 <row, x> row; turned back through shared memory
-        if (p.l2norm) {
-            put_dots(dq, sm.Q, sm.norm[0]);
-            put_dots(dk, sm.K, sm.norm[1]);
-        }
-        grad_sync();
-        __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(sm.S);
-        const auto finish = [&](const float (&x)[2][8], const uint8_t* tile, const float* inv, const float (*dots)[kC], __nv_bfloat16* to) {
-            float c[4] = {};
+            if (!last) {
+                __syncthreads();
+                ask(now, hv + 1, false);
+                ++it;
+                continue;
+            }
+            // through the norm of the rows: x - ||row||^-2 <row, x> row; turned back through shared memory
             if (p.l2norm) {
+                put_dots(dq, sm.Q, sm.norm[0]);
+                put_dots(dk, sm.K, sm.norm[1]);
+            }
+            grad_sync();
+            uint8_t* const out = &sm.r[1][0];  // two tiles of 64 x 128 in the 128-byte swizzle
+            const auto finish = [&](const float (&x)[2][8], const uint8_t* tile, const float* inv, const float (*dots)[kC], uint8_t* to) {
+                float c[4] = {};
+                if (p.l2norm) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int t = t0 + e / 2 * 8 + e % 2;
-                    c[e] = inv[t] * inv[t] * ((dots[0][t] + dots[1][t]) + (dots[2][t] + dots[3][t]));
+                    for (int e = 0; e < 4; e += 2) {
+                        const int t = t0 + e / 2 * 8;
+                        const float2 a = *reinterpret_cast<const float2*>(inv + t);
+                        float2 d[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) d[i] = *reinterpret_cast<const float2*>(dots[i] + t);
+                        c[e] = a.x * a.x * ((d[0].x + d[1].x) + (d[2].x + d[3].x)), c[e + 1] = a.y * a.y * ((d[0].y + d[1].y) + (d[2].y + d[3].y));
+                    }
+                }
+#pragma unroll
+                for (int lh = 0; lh < 2; ++lh) {
+                    uint32_t w[4];
+                    turned_swizzled(tile, quarter * 16, quad * 32 + lh * 16, w);
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2)
+                        w[i / 2] = pack_bf16x2(fmaf(-c[i / 4 * 2], bf16_lo(w[i / 2]), x[lh][i]), fmaf(-c[i / 4 * 2 + 1], bf16_hi(w[i / 2]), x[lh][i + 1]));
+                    const int lane = tid % 32, t = quarter * 16 + (lane & 7) + (lane >> 4) * 8, f = quad * 32 + lh * 16 + ((lane >> 3) & 1) * 8;
+                    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(smem_u32(to + f / 64 * kTile + swizzled(t, f % 64))), "r"(w[0]), "r"(w[1]),
+                                 "r"(w[2]), "r"(w[3])
+                                 : "memory");
+                }
+            };
+            finish(dq, sm.Q, sm.tab + TAB_RQ * kC, sm.norm[0], out);
+            finish(dk, sm.K, sm.tab + TAB_RK * kC, sm.norm[1], out + 2 * kTile);
+            __syncthreads();
+            const Unit next = units[(n + 1) & 1];
+            if (next.ok) ask(next, next.hk * heads, true);
+            const long long at = p.qk.at(s, first, now.hk);
+#pragma unroll
+            for (int i = tid; i < kC * kD / 8; i += kGradThreads) {
+                const int row = i / 16, col = i % 16 * 8, place = col / 64 * kTile + swizzled(row, col % 64);
+                if (row < rows) {
+                    *reinterpret_cast<uint4*>(p.dQ + at + row * p.qk.token + col) = *reinterpret_cast<const uint4*>(out + place);
+                    *reinterpret_cast<uint4*>(p.dK + at + row * p.qk.token + col) = *reinterpret_cast<const uint4*>(out + 2 * kTile + place);
                 }
             }
 #pragma unroll
-            for (int lh = 0; lh < 2; ++lh) {
-                uint32_t w[4];
-                turned_swizzled(tile, quarter * 16, quad * 32 + lh * 16, w);
-#pragma unroll
-                for (int i = 0; i < 8; i += 2)
-                    w[i / 2] = pack_bf16x2(fmaf(-c[i / 4 * 2], bf16_lo(w[i / 2]), x[lh][i]), fmaf(-c[i / 4 * 2 + 1], bf16_hi(w[i / 2]), x[lh][i + 1]));
-                const int lane = tid % 32;
-                const uint32_t at = smem_u32(to + (quarter * 16 + (lane & 7) + (lane >> 4) * 8) * kLdX + quad * 32 + lh * 16 + ((lane >> 3) & 1) * 8);
-                asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-            }
-        };
-        finish(dq, sm.Q, sm.tab + TAB_RQ * kC, sm.norm[0], out);
-        finish(dk, sm.K, sm.tab + TAB_RK * kC, sm.norm[1], out + kC * kLdX);
-        grad_sync();
-        const long long at = p.qk.at(s, first, hk);
-        for (int i = tid; i < kC * kD / 8; i += kGradThreads) {
-            const int row = i / 16, col = i % 16 * 8;
-            if (row < rows) {
-                *reinterpret_cast<uint4*>(p.dQ + at + row * p.qk.token + col) = *reinterpret_cast<const uint4*>(out + row * kLdX + col);
-                *reinterpret_cast<uint4*>(p.dK + at + row * p.qk.token + col) = *reinterpret_cast<const uint4*>(out + (kC + row) * kLdX + col);
-            }
+            for (int i = 0; i < 16; ++i) (&dq[0][0])[i] = (&dk[0][0])[i] = 0.f;
+            now = next;
+            it = 0;
+            ++n;
         }
     }
     if (failed) *p.status = GDN_ERR_TIMEOUT;
@@ -1469,12 +1530,13 @@ int launch_layer_backward(const ProblemB& q, cudaStream_t stream) {
     };
     p.qk = strides(q.H_k, kD), p.v = strides(q.H_v, kD), p.gate = strides(q.H_v, 1);
     const long long places = packed ? chunk_places(q.n_seq, q.T) : static_cast<long long>(q.n_seq) * p.chunks;
+    p.units = places * q.H_k;
     const long long chains = static_cast<long long>(q.n_seq) * q.H_v;
     if (places * q.H_k >= (1LL << 31) || chains >= (1LL << 31)) return GDN_ERR_UNSUPPORTED;
     const bool ok = launch<SmemSystem>(chunk_system_kernel, places * q.H_k, kThreads, p, stream) &&
                     launch<SmemF>(chunk_states_kernel, chains, kChainThreads, p, stream) &&
                     launch<SmemB>(chunk_state_grads_kernel, chains, kChainThreads, p, stream) &&
-                    launch<SmemC>(chunk_grads_kernel, places * q.H_k, kGradThreads + 32, p, stream);
+                    launch<SmemC>(chunk_grads_kernel, p.units < kSMs ? p.units : kSMs, kGradThreads + 32, p, stream);
     return ok ? GDN_OK : GDN_ERR_LAUNCH;
 }
 
