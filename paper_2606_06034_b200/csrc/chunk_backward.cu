@@ -312,27 +312,13 @@ __global__ void __launch_bounds__(kThreads) chunk_system_kernel(const ParamsB p)
 // One CTA has a (sequence, value head). Everything is kept transposed, a feature of the value on each of the 128 lanes of tensor memory: S
 // and D [v x key], and z, u, y, r [v x token]. The fp32 operand of a product, split into three bf16 pieces, is A, in tensor memory; B is a tile in
 // shared memory: K or Q as they are (both ways round), T or P in pieces. All sums are fp32 in tensor memory; the state itself stays in registers
-// (64 values a thread) and takes the chunk's part, summed on its own, with one fma.
-// Eight warps: two for each quarter of the lanes, each with half of the columns. Registers have the layout of the 16 x 256 bit loads:
+// (32 values a thread) and takes the chunk's part, summed on its own, with one fma.
+// Sixteen warps: four for each quarter of the lanes, each with a quarter of the columns. Registers have the layout of the 16 x 256 bit loads:
 // row (lane / 4) and row + 8 of 16 lanes, columns 2 (lane mod 4) and the next of every 8. In it a warp's 8-byte stores fill whole sectors.
+constexpr int kWorkers = 512;  // threads that do what lies between the products
 constexpr int kLdT = 136;  // rows of the tiles that ldmatrix turns, in bf16: 272 bytes, no bank conflicts
 constexpr uint32_t kNegA = 1u << 13;  // instruction descriptor: A negated
 
-__device__ __forceinline__ void tm_ld64(uint32_t taddr, float (&x)[32]) {  // 16 lanes x 64 columns
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
-}
 __device__ __forceinline__ void tm_ld32(uint32_t taddr, float (&x)[16]) {  // 16 lanes x 32 columns
     uint32_t r[16];
     asm volatile(
@@ -345,18 +331,23 @@ __device__ __forceinline__ void tm_ld32(uint32_t taddr, float (&x)[16]) {  // 16
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
 }
-// the reverse for packed pairs: 16 lanes x 16 or 32 columns of pairs
+__device__ __forceinline__ void tm_ld16(uint32_t taddr, float (&x)[8]) {  // 16 lanes x 16 columns
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r[i]);
+}
+// the reverse for packed pairs: 16 lanes x 8 or 16 columns of pairs
+__device__ __forceinline__ void tm_st_pairs(uint32_t taddr, const uint32_t (&r)[4]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
 __device__ __forceinline__ void tm_st_pairs(uint32_t taddr, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
                  "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
-}
-__device__ __forceinline__ void tm_st_pairs(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-        "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
 }
 // 2 N values of 16 lanes, split, into the columns of the three pieces (`apart` columns from one piece to the next)
 template <int N>
@@ -431,11 +422,11 @@ __device__ __forceinline__ void publish() {
 // hand-offs: the computing warps arrive and go on, N threads wait. Each is passed once a chunk, and a barrier of the whole CTA lies between two chunks.
 template <int ID, int N = 32>
 __device__ __forceinline__ void arrive() {
-    asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kThreads + N) : "memory");
+    asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kWorkers + N) : "memory");
 }
 template <int ID, int N = 32>
 __device__ __forceinline__ void await() {
-    asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kThreads + N) : "memory");
+    asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kWorkers + N) : "memory");
 }
 
 // Products of the chains, each issued by one thread. A [128 lanes x K] in three pieces of K / 2 columns at `a`; the small ones first.
@@ -473,26 +464,23 @@ __device__ __forceinline__ void product_block(uint32_t d, uint32_t a, uint64_t b
 template <bool COLS>
 __device__ __forceinline__ void product_system(uint32_t d, uint32_t a, uint32_t tiles) {
     const uint64_t b = COLS ? desc_cols(tiles) : desc_rows(tiles);
-    bool more = false;
 #pragma unroll
-    for (int sum = 2; sum >= 0; --sum)
+    for (int q = 0; q < 4; ++q)  // (products of one shape in a row: a change of shape drains the pipe)
 #pragma unroll
-        for (int i = sum; i >= 0; --i) {
-            const int j = sum - i;  // the pieces of A and M; one middle piece: negated
+        for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                product_block<COLS>(d, a + i * 32, b + j * kTile / 16, COLS ? 3 - q : q, (i == 1) != (j == 1), more);
-                more = true;
+            for (int i = sum; i >= 0; --i) {
+                const int j = sum - i;  // the pieces of A and M; one middle piece: negated
+                product_block<COLS>(d, a + i * 32, b + j * kTile / 16, COLS ? 3 - q : q, (i == 1) != (j == 1), q > 0 || sum < 2 || i < 2);
             }
-        }
 }
 // d = A P, A [128 x 64 tokens] bf16, P lower triangular in three tiles
 __device__ __forceinline__ void product_pairs(uint32_t d, uint32_t a, uint32_t tiles) {
     const uint64_t b = desc_cols(tiles);
 #pragma unroll
-    for (int i = kPieces - 1; i >= 0; --i)
+    for (int k = 3; k >= 0; --k)
 #pragma unroll
-        for (int k = 3; k >= 0; --k) product_block<true>(d, a, b + i * kTile / 16, k, i == 1, i < kPieces - 1 || k < 3);
+        for (int i = kPieces - 1; i >= 0; --i) product_block<true>(d, a, b + i * kTile / 16, k, i == 1, k < 3 || i < kPieces - 1);
 }
 
 // a value for each of a thread's 8 x 2 rows and columns: `f(row, column, i)` gets the place of x[i], x[i + 1] (neighbouring columns)
@@ -504,21 +492,34 @@ __device__ __forceinline__ void for_pairs(const F& f) {
 }
 
 constexpr int kLoaders = 96;
-constexpr int kChainThreads = kThreads + 32 + kLoaders;  // eight warps that compute, one that issues the products, three that load and store tiles
+constexpr int kChainThreads = kWorkers + 32 + kLoaders;  // sixteen warps that compute, one that issues the products, three that load and store tiles
 constexpr int kImage = 2 * 2 * 2 * kTile;     // bytes of a state's tiles: two pieces of two tiles of 128 rows
 // Byte of element (row, col) of a state in its image
 __device__ __forceinline__ int image_at(int piece, int row, int col) { return (piece * 2 + col / 64) * 2 * kTile + swizzled(row, col % 64); }
 // this thread's part of a state (see for_pairs) into the image
-__device__ __forceinline__ void put_image(uint8_t* image, const float (&S)[2][32], int row0, int half) {
+__device__ __forceinline__ void put_image(uint8_t* image, const float (&S)[2][16], int row0, int quarter) {
 #pragma unroll
     for (int lh = 0; lh < 2; ++lh)
-        for_pairs<32>([&](int row, int col, int i) {
+        for_pairs<16>([&](int row, int col, int i) {
             const uint32_t h = pack_bf16x2(S[lh][i], S[lh][i + 1]);
             const uint32_t m = pack_bf16x2(bf16_minus_lo(h, S[lh][i]), bf16_minus_hi(h, S[lh][i + 1]));
-            uint8_t* const at = image + image_at(0, row0 + lh * 16 + row, half * 64 + col);
+            uint8_t* const at = image + image_at(0, row0 + lh * 16 + row, quarter * 32 + col);
             *reinterpret_cast<uint32_t*>(at) = h;
             *reinterpret_cast<uint32_t*>(at + kImage / 2) = m;
         });
+}
+
+// the sum over the lanes of a column group of four tokens' values; a lane gets that of token place l.g / 2
+__device__ __forceinline__ float token_sum(const float (&x)[4], const Lane& l) {
+    float a[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float keep = l.g & 4 ? x[2 + i] : x[i], give = l.g & 4 ? x[i] : x[2 + i];
+        a[i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+    }
+    const float keep = l.g & 2 ? a[1] : a[0], give = l.g & 2 ? a[0] : a[1];
+    const float b = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+    return b + __shfl_xor_sync(0xffffffffu, b, 4);
 }
 
 // tensor memory: the state's part of the chunk (128 columns), the state's pieces, z or u, the pieces of the right-hand side or of u
@@ -584,7 +585,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
     const int warp = threadIdx.x / 32;
     Chain ch;
     chain_begin(ch, bars, &base, kTmColumns);
-    if (warp == kThreads / 32) {  // ---- the products
+    if (warp == kWorkers / 32) {  // ---- the products
         for (int c = 0; c < n; ++c) {
             StageF& st = sm.stage[c % 2];
             const uint32_t tileK = smem_u32(st.K), tileT = smem_u32(st.T);
@@ -611,8 +612,8 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             }
             __syncwarp();
         }
-    } else if (warp > kThreads / 32) {  // ---- the tiles
-        const int me = threadIdx.x - kThreads - 32;
+    } else if (warp > kWorkers / 32) {  // ---- the tiles
+        const int me = threadIdx.x - kWorkers - 32;
         const auto load = [&](int c) {
             if (c < n) {
                 StageF& st = sm.stage[c % 2];
@@ -644,82 +645,80 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
         }
         tma_store_wait_all<0>();
     } else {  // ---- what lies between the products
-        const int half = warp / 4, row0 = warp % 4 * 32;
-        float S[2][32];
+        const int quarter = warp / 4, row0 = warp % 4 * 32;
+        float S[2][16];
         const long long state = (static_cast<long long>(s) * p.H_v + h) * kD * kD;
 #pragma unroll
         for (int lh = 0; lh < 2; ++lh)
-            for_pairs<32>([&](int row, int col, int i) {
+            for_pairs<16>([&](int row, int col, int i) {
                 const float2 x = p.S_in == nullptr ? make_float2(0.f, 0.f)
-                                                   : *reinterpret_cast<const float2*>(p.S_in + state + (row0 + lh * 16 + row) * kD + half * 64 + col);
+                                                   : *reinterpret_cast<const float2*>(p.S_in + state + (row0 + lh * 16 + row) * kD + quarter * 32 + col);
                 S[lh][i] = x.x, S[lh][i + 1] = x.y;
             });
         for (int c = 0; c < n; ++c) {
             const StageF& st = sm.stage[c % 2];
             float* const ws = chunk_ws(p, seq.slot + c, h);
 #pragma unroll
-            for (int lh = 0; lh < 2; ++lh) tm_st_split<16>(ch.tm + ch.lanes + (lh << 20) + kTmState + half * 32, 64, S[lh]);
+            for (int lh = 0; lh < 2; ++lh) tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmState + quarter * 16, 64, S[lh]);
             publish();
             if (__syncthreads_or(ch.failed)) break;
-            put_image(sm.image, S, row0, half);
+            put_image(sm.image, S, row0, quarter);
             fence_proxy_async_smem();
             arrive<3, kLoaders>();
-            uint32_t v[2][8];
+            uint32_t v[2][4];
 #pragma unroll
-            for (int lh = 0; lh < 2; ++lh)
-#pragma unroll
-                for (int q = 0; q < 2; ++q) turned(st.V, half * 32 + q * 16, row0 + lh * 16, reinterpret_cast<uint32_t(&)[4]>(v[lh][q * 4]));
+            for (int lh = 0; lh < 2; ++lh) turned(st.V, quarter * 16, row0 + lh * 16, v[lh]);
             ch.wait();
-            float z[2][16];
+            float z[2][8];
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float x[16];
-                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, z[lh]);
+                float x[8];
+                tm_ld16(ch.tm + ch.lanes + (lh << 20) + kTmAcc + quarter * 16, z[lh]);
                 tmem_wait_ld();
-                for_pairs<16>([&](int, int col, int i) {
-                    const int t = half * 32 + col;
+                for_pairs<8>([&](int, int col, int i) {
+                    const int t = quarter * 16 + col;
                     const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_EGK * kC + t), b = *reinterpret_cast<const float2*>(st.tab + TAB_BETA * kC + t);
                     z[lh][i] *= e.x, z[lh][i + 1] *= e.y;
                     x[i] = b.x * (bf16_lo(v[lh][i / 2]) - z[lh][i]), x[i + 1] = b.y * (bf16_hi(v[lh][i / 2]) - z[lh][i + 1]);
                 });
-                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmRhs + half * 16, 32, x);
+                tm_st_split<4>(ch.tm + ch.lanes + (lh << 20) + kTmRhs + quarter * 8, 32, x);
             }
             publish();
             arrive<1>();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
-                for_pairs<16>([&](int row, int col, int i) {
-                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + half * 32 + col) = make_float2(z[lh][i], z[lh][i + 1]);
+                for_pairs<8>([&](int row, int col, int i) {
+                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + quarter * 16 + col) = make_float2(z[lh][i], z[lh][i + 1]);
                 });
             ch.wait();
-            float u[2][16];
+            float u[2][8];
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float x[16];
-                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, u[lh]);
+                float x[8];
+                tm_ld16(ch.tm + ch.lanes + (lh << 20) + kTmAcc + quarter * 16, u[lh]);
                 tmem_wait_ld();
-                for_pairs<16>([&](int, int col, int i) {
-                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_ECK * kC + half * 32 + col);
+                for_pairs<8>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_ECK * kC + quarter * 16 + col);
                     x[i] = u[lh][i] * e.x, x[i + 1] = u[lh][i + 1] * e.y;
                 });
-                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmRhs + half * 16, 32, x);
+                tm_st_split<4>(ch.tm + ch.lanes + (lh << 20) + kTmRhs + quarter * 8, 32, x);
             }
             publish();
             arrive<2>();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
-                for_pairs<16>([&](int row, int col, int i) {
-                    *reinterpret_cast<float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + half * 32 + col) = make_float2(u[lh][i], u[lh][i + 1]);
+                for_pairs<8>([&](int row, int col, int i) {
+                    *reinterpret_cast<float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + quarter * 16 + col) = make_float2(u[lh][i], u[lh][i + 1]);
                 });
             const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
             ch.wait();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float x[32];
-                tm_ld64(ch.tm + ch.lanes + (lh << 20) + kTmDelta + half * 64, x);
+                float x[16];
+                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmDelta + quarter * 32, x);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) S[lh][i] = fmaf(decay, S[lh][i], x[i]);
+                for (int i = 0; i < 16; ++i) S[lh][i] = fmaf(decay, S[lh][i], x[i]);
             }
         }
     }
@@ -754,7 +753,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
     const int warp = threadIdx.x / 32;
     Chain ch;
     chain_begin(ch, bars, &base, kTmColumns);
-    if (warp == kThreads / 32) {  // ---- the products
+    if (warp == kWorkers / 32) {  // ---- the products
         uint32_t turn = 0;
         for (int c = n - 1; c >= 0; --c) {
             StageB& st = sm.stage[c % 2];
@@ -791,8 +790,8 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             }
             __syncwarp();
         }
-    } else if (warp > kThreads / 32) {  // ---- the tiles
-        const int me = threadIdx.x - kThreads - 32;
+    } else if (warp > kWorkers / 32) {  // ---- the tiles
+        const int me = threadIdx.x - kWorkers - 32;
         uint32_t turn = 0;
         const auto load = [&](int c) {
             if (c >= 0) {
@@ -834,125 +833,110 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
         }
         tma_store_wait_all<0>();
     } else {  // ---- what lies between the products
-        const int half = warp / 4, row0 = warp % 4 * 32;
+        const int quarter = warp / 4, row0 = warp % 4 * 32;
         const Lane l;
-        float D[2][32];
+        float D[2][16];
         const long long state = (static_cast<long long>(s) * p.H_v + h) * kD * kD;
 #pragma unroll
         for (int lh = 0; lh < 2; ++lh)
-            for_pairs<32>([&](int row, int col, int i) {
+            for_pairs<16>([&](int row, int col, int i) {
                 const float2 x = p.dS_out == nullptr ? make_float2(0.f, 0.f)
-                                                     : *reinterpret_cast<const float2*>(p.dS_out + state + (row0 + lh * 16 + row) * kD + half * 64 + col);
+                                                     : *reinterpret_cast<const float2*>(p.dS_out + state + (row0 + lh * 16 + row) * kD + quarter * 32 + col);
                 D[lh][i] = x.x, D[lh][i + 1] = x.y;
             });
         for (int c = n - 1; c >= 0; --c) {
             const StageB& st = sm.stage[c % 2];
             float* const ws = chunk_ws(p, seq.slot + c, h);
 #pragma unroll
-            for (int lh = 0; lh < 2; ++lh) tm_st_split<16>(ch.tm + ch.lanes + (lh << 20) + kTmState + half * 32, 64, D[lh]);
+            for (int lh = 0; lh < 2; ++lh) tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmState + quarter * 16, 64, D[lh]);
             publish();
             if (__syncthreads_or(ch.failed)) break;
-            float2 u[2][8];
+            float2 u[2][4];
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {  // dO, its features on the lanes
-                uint32_t w[8];
-                turned(st.dO, half * 32, row0 + lh * 16, reinterpret_cast<uint32_t(&)[4]>(w[0]));
-                turned(st.dO, half * 32 + 16, row0 + lh * 16, reinterpret_cast<uint32_t(&)[4]>(w[4]));
-                tm_st_pairs(ch.tm + ch.lanes + (lh << 20) + kTmO + half * 16, w);
+                uint32_t w[4];
+                turned(st.dO, quarter * 16, row0 + lh * 16, w);
+                tm_st_pairs(ch.tm + ch.lanes + (lh << 20) + kTmO + quarter * 8, w);
             }
             publish();
             arrive<1>();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
-                for_pairs<16>([&](int row, int col, int i) {
-                    u[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + half * 32 + col);
+                for_pairs<8>([&](int row, int col, int i) {
+                    u[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + quarter * 16 + col);
                 });
-            put_image(sm.image, D, row0, half);
+            put_image(sm.image, D, row0, quarter);
             fence_proxy_async_smem();
             arrive<5, kLoaders>();
             ch.wait();
-            float dots[kDots][8] = {};  // of this thread's eight tokens: 8 (i / 4) + 2 c + e at [i / 4 * 2 + e]
+            float dots[kDots][4] = {};  // of this thread's four tokens: 8 (i / 4) + 2 c + e at [i / 4 * 2 + e]
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float y[16], x[16];
-                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, y);
-                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmX + half * 32, x);
+                float y[8], x[8];
+                tm_ld16(ch.tm + ch.lanes + (lh << 20) + kTmAcc + quarter * 16, y);
+                tm_ld16(ch.tm + ch.lanes + (lh << 20) + kTmX + quarter * 16, x);
                 tmem_wait_ld();
-                for_pairs<16>([&](int, int col, int i) {
-                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_ECK * kC + half * 32 + col);
+                for_pairs<8>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_ECK * kC + quarter * 16 + col);
                     const float y0 = e.x * y[i], y1 = e.y * y[i + 1];
                     dots[1][i / 4 * 2] = fmaf(u[lh][i / 2].x, y0, dots[1][i / 4 * 2]);
                     dots[1][i / 4 * 2 + 1] = fmaf(u[lh][i / 2].y, y1, dots[1][i / 4 * 2 + 1]);
                     x[i] += y0, x[i + 1] += y1;
                 });
-                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmDu + half * 16, 32, x);
+                tm_st_split<4>(ch.tm + ch.lanes + (lh << 20) + kTmDu + quarter * 8, 32, x);
             }
             publish();
             arrive<2>();
-            float2 z[2][8];
+            float2 z[2][4];
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
-                for_pairs<16>([&](int row, int col, int i) {
-                    z[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + half * 32 + col);
+                for_pairs<8>([&](int row, int col, int i) {
+                    z[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + quarter * 16 + col);
                 });
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float x[16];
-                uint32_t w[2][4];
-                turned(st.dO, half * 32, row0 + lh * 16, w[0]);
-                turned(st.dO, half * 32 + 16, row0 + lh * 16, w[1]);
-                for_pairs<16>([&](int, int col, int i) {
-                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_SEGQ * kC + half * 32 + col);
-                    const uint32_t o = w[i / 8][i % 8 / 2];
+                float x[8];
+                uint32_t w[4];
+                turned(st.dO, quarter * 16, row0 + lh * 16, w);
+                for_pairs<8>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_SEGQ * kC + quarter * 16 + col);
+                    const uint32_t o = w[i / 2];
                     x[i] = e.x * bf16_lo(o), x[i + 1] = e.y * bf16_hi(o);
                 });
-                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmW + half * 16, 32, x);
+                tm_st_split<4>(ch.tm + ch.lanes + (lh << 20) + kTmW + quarter * 8, 32, x);
             }
             publish();
             arrive<3>();
             ch.wait();  // (for r; what was issued behind it may still run)
             arrive<6, kLoaders>();
-            float r[2][16];
+            float r[2][8];
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float x[16];
-                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmAcc + half * 32, r[lh]);
+                float x[8];
+                tm_ld16(ch.tm + ch.lanes + (lh << 20) + kTmAcc + quarter * 16, r[lh]);
                 tmem_wait_ld();
-                for_pairs<16>([&](int, int col, int i) {
-                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_BEGK * kC + half * 32 + col);
+                for_pairs<8>([&](int, int col, int i) {
+                    const float2 e = *reinterpret_cast<const float2*>(st.tab + TAB_BEGK * kC + quarter * 16 + col);
                     x[i] = -e.x * r[lh][i], x[i + 1] = -e.y * r[lh][i + 1];
                 });
-                tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmDu + half * 16, 32, x);
+                tm_st_split<4>(ch.tm + ch.lanes + (lh << 20) + kTmDu + quarter * 8, 32, x);
             }
             publish();
             arrive<4>();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
-                for_pairs<16>([&](int row, int col, int i) {
+                for_pairs<8>([&](int row, int col, int i) {
                     dots[0][i / 4 * 2] = fmaf(r[lh][i], z[lh][i / 2].x, dots[0][i / 4 * 2]);
                     dots[0][i / 4 * 2 + 1] = fmaf(r[lh][i + 1], z[lh][i / 2].y, dots[0][i / 4 * 2 + 1]);
-                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + half * 32 + col) = make_float2(r[lh][i], r[lh][i + 1]);
+                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + quarter * 16 + col) = make_float2(r[lh][i], r[lh][i + 1]);
                 });
-            // the tokens' sums over this warp's 32 features: lanes of one column group trade halves of their tokens
 #pragma unroll
             for (int d = 0; d < kDots; ++d) {
-                float a[4], b[2];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float keep = l.g & 4 ? dots[d][4 + i] : dots[d][i], give = l.g & 4 ? dots[d][i] : dots[d][4 + i];
-                    a[i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float keep = l.g & 2 ? a[2 + i] : a[i], give = l.g & 2 ? a[i] : a[2 + i];
-                    b[i] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
-                }
-                const float keep = l.g & 1 ? b[1] : b[0], give = l.g & 1 ? b[0] : b[1];
-                // (the bits of l.g are those of the token's place)
-                sm.dots[warp % 4][d][half * 32 + (l.g >> 1) * 8 + 2 * l.c + (l.g & 1)] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
+                const float sum = token_sum(dots[d], l);
+                if ((l.g & 1) == 0) sm.dots[warp % 4][d][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
             }
             const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
-            asm volatile("bar.sync 7, %0;" ::"n"(kThreads) : "memory");
+            asm volatile("bar.sync 7, %0;" ::"n"(kWorkers) : "memory");
             if (threadIdx.x < kDots * kC) {
                 const float* const at = &sm.dots[0][0][threadIdx.x];
                 ws[kWsDots + threadIdx.x] = (at[0] + at[kDots * kC]) + (at[2 * kDots * kC] + at[3 * kDots * kC]);
@@ -960,18 +944,18 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             ch.wait();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float x[32];
-                tm_ld64(ch.tm + ch.lanes + (lh << 20) + kTmDelta + half * 64, x);
+                float x[16];
+                tm_ld32(ch.tm + ch.lanes + (lh << 20) + kTmDelta + quarter * 32, x);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) D[lh][i] = fmaf(decay, D[lh][i], x[i]);
+                for (int i = 0; i < 16; ++i) D[lh][i] = fmaf(decay, D[lh][i], x[i]);
             }
         }
         if (p.dS_in != nullptr) {
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
-                for_pairs<32>([&](int row, int col, int i) {
-                    *reinterpret_cast<float2*>(p.dS_in + state + (row0 + lh * 16 + row) * kD + half * 64 + col) = make_float2(D[lh][i], D[lh][i + 1]);
+                for_pairs<16>([&](int row, int col, int i) {
+                    *reinterpret_cast<float2*>(p.dS_in + state + (row0 + lh * 16 + row) * kD + quarter * 32 + col) = make_float2(D[lh][i], D[lh][i + 1]);
                 });
         }
     }
@@ -1001,15 +985,6 @@ struct Unit {  // what a CTA takes next: a chunk of a key head
     int ok, slot, hk, s, first, rows;
 };
 
-__device__ __forceinline__ void tm_ld16(uint32_t taddr, float (&x)[8]) {  // 16 lanes x 16 columns
-    uint32_t r[8];
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(taddr)
-                 : "memory");
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r[i]);
-}
 __device__ __forceinline__ void ldmatrix_turned(uint32_t at, uint32_t (&w)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
 }
@@ -1017,18 +992,6 @@ __device__ __forceinline__ void ldmatrix_turned(uint32_t at, uint32_t (&w)[4]) {
 __device__ __forceinline__ void turned_swizzled(const uint8_t* tile, int t0, int v0, uint32_t (&w)[4]) {
     const int lane = threadIdx.x % 32, t = t0 + (lane & 7) + (lane >> 4) * 8, v = v0 + ((lane >> 3) & 1) * 8;
     ldmatrix_turned(smem_u32(tile + v / 64 * kTile + swizzled(t, v % 64)), w);
-}
-// the sum over the lanes of a column group of four tokens' values; a lane gets that of token place l.g / 2
-__device__ __forceinline__ float token_sum(const float (&x)[4], const Lane& l) {
-    float a[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float keep = l.g & 4 ? x[2 + i] : x[i], give = l.g & 4 ? x[i] : x[2 + i];
-        a[i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
-    }
-    const float keep = l.g & 2 ? a[1] : a[0], give = l.g & 2 ? a[0] : a[1];
-    const float b = keep + __shfl_xor_sync(0xffffffffu, give, 8);
-    return b + __shfl_xor_sync(0xffffffffu, b, 4);
 }
 template <int ID>
 __device__ __forceinline__ void grad_arrive() {
