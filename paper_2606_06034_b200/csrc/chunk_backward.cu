@@ -24,6 +24,8 @@
 // Precision: dbeta, dg and dS_in are fp32 and so is what they are made of. Products run on the tensor cores in tf32 with an fp32
 // operand as the sum of its upper 11 bits and the rest (2 products where the other operand is bf16, which tf32 holds exactly, 3 where
 // both are fp32): 2^-21 of a product is lost. What only reaches dQ, dK, dV, which are rounded to bf16 (2^-9), takes one product.
+#include <cuda.h>
+
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 
@@ -65,7 +67,13 @@ struct ParamsB {
     long long units;                        // places of chunks in the workspace times key heads
     Strides qk, v, gate;
     float scale;
-    bool l2norm;
+    bool l2norm, token_major;
+};
+
+// The token tensors for the copy engine: [heads][tokens][128], or [batch][tokens][heads x 128] where they are token-major; boxes of 64 x 64
+// in the 128-byte swizzle
+struct Maps {
+    CUtensorMap Q, K, V, dO;
 };
 
 // Sequence s: its first token, its length and the index of its first chunk in the workspace. Packed: sequence s starts at cu[s] / 64 +
@@ -316,7 +324,6 @@ __global__ void __launch_bounds__(kThreads) chunk_system_kernel(const ParamsB p)
 // Sixteen warps: four for each quarter of the lanes, each with a quarter of the columns. Registers have the layout of the 16 x 256 bit loads:
 // row (lane / 4) and row + 8 of 16 lanes, columns 2 (lane mod 4) and the next of every 8. In it a warp's 8-byte stores fill whole sectors.
 constexpr int kWorkers = 512;  // threads that do what lies between the products
-constexpr int kLdT = 136;  // rows of the tiles that ldmatrix turns, in bf16: 272 bytes, no bank conflicts
 constexpr uint32_t kNegA = 1u << 13;  // instruction descriptor: A negated
 
 __device__ __forceinline__ void tm_ld32(uint32_t taddr, float (&x)[16]) {  // 16 lanes x 32 columns
@@ -359,35 +366,28 @@ __device__ __forceinline__ void tm_st_split(uint32_t taddr, uint32_t apart, cons
     tm_st_pairs(taddr + apart, m);
     tm_st_pairs(taddr + 2 * apart, l);
 }
-// [token][feature] rows turned: four 8 x 8 blocks, tokens t0 .. t0 + 15 and features v0 .. v0 + 15, as pairs of tokens: w[0], w[1] features
-// v0 .. and v0 + 8 .. of the first 8 tokens, w[2], w[3] of the others (the layout of the accumulators' registers)
-__device__ __forceinline__ void turned(const __nv_bfloat16* tile, int t0, int v0, uint32_t (&w)[4]) {
-    const int lane = threadIdx.x % 32;
-    const uint32_t at = smem_u32(tile + (t0 + (lane & 7) + (lane >> 4) * 8) * kLdT + v0 + ((lane >> 3) & 1) * 8);
+__device__ __forceinline__ void ldmatrix_turned(uint32_t at, uint32_t (&w)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
 }
-// 64 rows of 128 bf16 by N threads: as two tiles of 64 x 64 in the 128-byte swizzle, `apart` bytes from one to the other / as rows of kLdT;
-// rows from `rows` on are zeros
-template <int N>
-__device__ __forceinline__ void copy_tile(uint8_t* dst, const __nv_bfloat16* src, long long row_stride, int rows, int me, int apart = kTile) {
-    static_assert(N % 16 == 0, "");
-    const int c = me % 16 * 8;
-    src += me / 16 * row_stride + c;
-    dst += c / 64 * apart;
-#pragma unroll 8
-    for (int r = me / 16; r < kC; r += N / 16) {
-        cp16(dst + swizzled(r, c % 64), r < rows ? src : src - (r - me / 16) * row_stride - me / 16 * row_stride, r < rows);
-        src += N / 16 * row_stride;
-    }
+// [token][feature] rows turned: four 8 x 8 blocks, tokens t0 .. t0 + 15 and features v0 .. v0 + 15, as pairs of tokens: w[0], w[1] features
+// v0 .. and v0 + 8 .. of the first 8 tokens, w[2], w[3] of the others (the layout of the accumulators' registers)
+__device__ __forceinline__ void turned(const uint8_t* tile, int t0, int v0, uint32_t (&w)[4]) {
+    const int lane = threadIdx.x % 32, t = t0 + (lane & 7) + (lane >> 4) * 8, v = v0 + ((lane >> 3) & 1) * 8;
+    ldmatrix_turned(smem_u32(tile + v / 64 * kTile + swizzled(t, v % 64)), w);
 }
+// 64 tokens of 128 bf16 as two 64 x 64 tiles in the 128-byte swizzle; one thread asks. A box takes what lies behind a sequence's end too:
+// those rows are cleared when it has come (clear_tail), for 0 times what is there need not be 0.
+__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap& map, const ParamsB& p, int heads, int s, int t, int h, uint64_t* bar) {
+    const int x = p.token_major ? h * kD : 0, z = p.cu != nullptr ? (p.token_major ? 0 : h) : (p.token_major ? s : s * heads + h);
+    tma_load_3d(dst, &map, bar, x, t, z);
+    tma_load_3d(dst + kTile, &map, bar, x + 64, t, z);
+}
+// rows from `rows` on of a tile, by N threads
 template <int N>
-__device__ __forceinline__ void copy_plain(__nv_bfloat16* dst, const __nv_bfloat16* src, long long row_stride, int rows, int me) {
-    const int c = me % 16 * 8;
-    src += me / 16 * row_stride + c;
-#pragma unroll 8
-    for (int r = me / 16; r < kC; r += N / 16) {
-        cp16(dst + r * kLdT + c, r < rows ? src : src - (r - me / 16) * row_stride - me / 16 * row_stride, r < rows);
-        src += N / 16 * row_stride;
+__device__ __forceinline__ void clear_tail(uint8_t* tile, int rows, int me) {
+    for (int i = rows * 8 + me; i < kC * 8; i += N) {
+        reinterpret_cast<uint4*>(tile)[i] = make_uint4(0u, 0u, 0u, 0u);
+        reinterpret_cast<uint4*>(tile + kTile)[i] = make_uint4(0u, 0u, 0u, 0u);
     }
 }
 // whole runs of bytes (multiples of 16): one thread asks, the copy engine does it
@@ -491,8 +491,8 @@ __device__ __forceinline__ void for_pairs(const F& f) {
     for (int i = 0; i < N; i += 2) f(l.g + ((i >> 1) & 1) * 8, (i >> 2) * 8 + 2 * l.c, i);
 }
 
-constexpr int kLoaders = 96;
-constexpr int kChainThreads = kWorkers + 32 + kLoaders;  // sixteen warps that compute, one that issues the products, three that load and store tiles
+constexpr int kLoaders = 32;
+constexpr int kChainThreads = kWorkers + 32 + kLoaders;  // sixteen warps that compute, one that issues the products, one that asks for tiles and has them stored
 constexpr int kImage = 2 * 2 * 2 * kTile;     // bytes of a state's tiles: two pieces of two tiles of 128 rows
 // Byte of element (row, col) of a state in its image
 __device__ __forceinline__ int image_at(int piece, int row, int col) { return (piece * 2 + col / 64) * 2 * kTile + swizzled(row, col % 64); }
@@ -563,18 +563,16 @@ __device__ __forceinline__ void chain_end(Chain& ch, int* status, uint32_t colum
 
 // Forward: z, u and the state at the start of every chunk. A chunk's chain is three products (24 of 128 x 64 x 16 each) and, between them, the
 // splitting of what the next one reads: z -> right-hand side -> u -> state. What goes to memory (the state, z, u) goes while products run.
-struct StageF {
-    uint8_t K[2 * kTile], T[kPieces * kTile];
+struct StageF {  // (the tiles lie on 1 KB)
+    uint8_t K[2 * kTile], V[2 * kTile], T[kPieces * kTile];
     float tab[kTabs * kC];
-    __nv_bfloat16 V[kC * kLdT];
-    uint8_t pad[1024 - (kC * kLdT * 2 + kTabs * kC * 4) % 1024];  // the tiles lie on 1 KB
 };
 struct SmemF {
     StageF stage[2];
     uint8_t image[kImage];
 };
 
-__global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const ParamsB p) {
+__global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const ParamsB p, const __grid_constant__ Maps maps) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SmemF& sm = *reinterpret_cast<SmemF*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
     __shared__ uint64_t bars[2];
@@ -615,25 +613,26 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
     } else if (warp > kWorkers / 32) {  // ---- the tiles
         const int me = threadIdx.x - kWorkers - 32;
         const auto load = [&](int c) {
-            if (c < n) {
+            if (c < n && me == 0) {
                 StageF& st = sm.stage[c % 2];
                 const float* const ws = chunk_ws(p, seq.slot + c, h);
-                if (me == 0) {
-                    mbar_arrive_expect_tx(ch.full, sizeof(st.T) + sizeof(st.tab));
-                    bulk_load(st.T, ws + kWsT, sizeof(st.T), ch.full);
-                    bulk_load(st.tab, ws + kWsTab, sizeof(st.tab), ch.full);
-                }
-                copy_tile<kLoaders>(st.K, p.K + p.qk.at(s, seq.first + c * kC, hk), p.qk.token, seq.len - c * kC, me);
-                copy_plain<kLoaders>(st.V, p.V + p.v.at(s, seq.first + c * kC, h), p.v.token, seq.len - c * kC, me);
-                cp_commit();
+                mbar_arrive_expect_tx(ch.full, sizeof(StageF));
+                load_tile(st.K, maps.K, p, p.H_k, s, seq.first + c * kC, hk, ch.full);
+                load_tile(st.V, maps.V, p, p.H_v, s, seq.first + c * kC, h, ch.full);
+                bulk_load(st.T, ws + kWsT, sizeof(st.T), ch.full);
+                bulk_load(st.tab, ws + kWsTab, sizeof(st.tab), ch.full);
             }
+            __syncwarp();
         };
         load(0);
         for (int c = 0; c < n; ++c) {
-            cp_wait<0>();
             tma_store_wait_read<0>();  // the image may be written again
-            fence_proxy_async_smem();
             ch.failed |= !wait_products(ch.full, c & 1);
+            if (seq.len - c * kC < kC) {
+                clear_tail<kLoaders>(sm.stage[c % 2].K, seq.len - c * kC, me);
+                clear_tail<kLoaders>(sm.stage[c % 2].V, seq.len - c * kC, me);
+                fence_proxy_async_smem();
+            }
             if (__syncthreads_or(ch.failed)) break;
             load(c + 1);
             await<3, kLoaders>();
@@ -727,10 +726,8 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
 
 // Backward: r and the state's gradient at the end of every chunk.
 struct StageB {
-    uint8_t K[2 * kTile], Q[2 * kTile];
+    uint8_t K[2 * kTile], Q[2 * kTile], dO[2 * kTile];
     float tab[kTabs * kC];
-    __nv_bfloat16 dO[kC * kLdT];
-    uint8_t pad[1024 - (kC * kLdT * 2 + kTabs * kC * 4) % 1024];
 };
 struct SmemB {
     StageB stage[2];
@@ -742,7 +739,7 @@ struct SmemB {
 // exp(g) dO (96); y or r; P^T dO; dO
 constexpr uint32_t kTmDu = kTmState, kTmW = kTmState + 96, kTmX = 384, kTmO = 448;
 
-__global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(const ParamsB p) {
+__global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(const ParamsB p, const __grid_constant__ Maps maps) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SmemB& sm = *reinterpret_cast<SmemB*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
     __shared__ uint64_t bars[2];
@@ -793,33 +790,34 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
     } else if (warp > kWorkers / 32) {  // ---- the tiles
         const int me = threadIdx.x - kWorkers - 32;
         uint32_t turn = 0;
+        // K, Q, dO have two stages; T and P one: they are asked for behind their last product of the chunk before
         const auto load = [&](int c) {
-            if (c >= 0) {
+            if (c >= 0 && me == 0) {
                 StageB& st = sm.stage[c % 2];
-                const int t = seq.first + c * kC, rows = seq.len - c * kC;
-                copy_tile<kLoaders>(st.K, p.K + p.qk.at(s, t, hk), p.qk.token, rows, me);
-                copy_tile<kLoaders>(st.Q, p.Q + p.qk.at(s, t, hk), p.qk.token, rows, me);
-                copy_plain<kLoaders>(st.dO, p.dO + p.v.at(s, t, h), p.v.token, rows, me);
-                cp_commit();
+                mbar_arrive_expect_tx(ch.full, sizeof(StageB) + sizeof(sm.T) + sizeof(sm.P));
+                load_tile(st.K, maps.K, p, p.H_k, s, seq.first + c * kC, hk, ch.full);
+                load_tile(st.Q, maps.Q, p, p.H_k, s, seq.first + c * kC, hk, ch.full);
+                load_tile(st.dO, maps.dO, p, p.H_v, s, seq.first + c * kC, h, ch.full);
+                bulk_load(st.tab, chunk_ws(p, seq.slot + c, h) + kWsTab, sizeof(st.tab), ch.full);
             }
+            __syncwarp();
         };
         const auto load_system = [&](int c) {
-            if (c >= 0 && me == 0) {
-                const float* const ws = chunk_ws(p, seq.slot + c, h);
-                mbar_arrive_expect_tx(ch.full, sizeof(sm.T) + sizeof(sm.P) + sizeof(sm.stage[0].tab));
-                bulk_load(sm.T, ws + kWsT, sizeof(sm.T) + sizeof(sm.P), ch.full);
-                bulk_load(sm.stage[c % 2].tab, ws + kWsTab, sizeof(sm.stage[0].tab), ch.full);
-            }
+            if (c >= 0 && me == 0) bulk_load(sm.T, chunk_ws(p, seq.slot + c, h) + kWsT, sizeof(sm.T) + sizeof(sm.P), ch.full);
             __syncwarp();
         };
         load(n - 1);
         load_system(n - 1);
         for (int c = n - 1; c >= 0; --c) {
-            cp_wait<0>();
             tma_store_wait_read<0>();
-            fence_proxy_async_smem();
             ch.failed |= !wait_products(ch.full, turn);
             turn ^= 1;
+            if (seq.len - c * kC < kC) {
+                clear_tail<kLoaders>(sm.stage[c % 2].K, seq.len - c * kC, me);
+                clear_tail<kLoaders>(sm.stage[c % 2].Q, seq.len - c * kC, me);
+                clear_tail<kLoaders>(sm.stage[c % 2].dO, seq.len - c * kC, me);
+                fence_proxy_async_smem();
+            }
             if (__syncthreads_or(ch.failed)) break;
             load(c - 1);
             await<5, kLoaders>();
@@ -985,14 +983,6 @@ struct Unit {  // what a CTA takes next: a chunk of a key head
     int ok, slot, hk, s, first, rows;
 };
 
-__device__ __forceinline__ void ldmatrix_turned(uint32_t at, uint32_t (&w)[4]) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-}
-// `turned` from a tile pair in the 128-byte swizzle
-__device__ __forceinline__ void turned_swizzled(const uint8_t* tile, int t0, int v0, uint32_t (&w)[4]) {
-    const int lane = threadIdx.x % 32, t = t0 + (lane & 7) + (lane >> 4) * 8, v = v0 + ((lane >> 3) & 1) * 8;
-    ldmatrix_turned(smem_u32(tile + v / 64 * kTile + swizzled(t, v % 64)), w);
-}
 template <int ID>
 __device__ __forceinline__ void grad_arrive() {
     asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kGradThreads + 32) : "memory");
@@ -1018,10 +1008,10 @@ __host__ __device__ constexpr uint32_t grad_idesc(int m, bool a_down, bool b_dow
 }
 constexpr uint32_t kTmDOS = 0, kTmRS = 64, kTmUD = 128, kTmDQ = 192, kTmDK = 256, kTmOU = 320, kTmRU = 384, kTmKK = kTmDQ, kTmQK = kTmDK;
 
-__global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const ParamsB p) {
+__global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const ParamsB p, const __grid_constant__ Maps maps) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SmemC& sm = *reinterpret_cast<SmemC*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
-    __shared__ uint64_t bar_pair, bar_s, bar_out, bar_d, bar_load;
+    __shared__ uint64_t bar_pair, bar_s, bar_out, bar_d, bar_load, bar_tile;
     __shared__ uint32_t base;
     __shared__ Unit units[2];
     const int tid = threadIdx.x, warp = tid / 32;
@@ -1041,7 +1031,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
     };
     if (tid == 0) {
         units[0] = find_unit(blockIdx.x);
-        for (uint64_t* b : {&bar_pair, &bar_s, &bar_out, &bar_d, &bar_load}) mbar_init(b, 1);
+        for (uint64_t* b : {&bar_pair, &bar_s, &bar_out, &bar_d, &bar_load, &bar_tile}) mbar_init(b, 1);
         mbar_fence_init();
     }
     if (warp == 0) {
@@ -1080,9 +1070,24 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             }
             __syncwarp();
         };
+        const auto load_tiles = [&](const Unit& x, int hv, bool keys) {
+            if (elect_one()) {
+                mbar_arrive_expect_tx(&bar_tile, (keys ? 3 : 1) * 2 * kTile + sizeof(sm.tab));
+                if (keys) {
+                    load_tile(sm.K, maps.K, p, p.H_k, x.s, x.first, x.hk, &bar_tile);
+                    load_tile(sm.Q, maps.Q, p, p.H_k, x.s, x.first, x.hk, &bar_tile);
+                }
+                load_tile(sm.dO, maps.dO, p, p.H_v, x.s, x.first, hv, &bar_tile);
+                bulk_load(sm.tab, chunk_ws(p, x.slot, hv) + kWsTab, sizeof(sm.tab), &bar_tile);
+            }
+            __syncwarp();
+        };
         uint32_t phase = 0;
         Unit now = units[0];
-        if (now.ok) load(chunk_ws(p, now.slot, now.hk * heads));
+        if (now.ok) {
+            load(chunk_ws(p, now.slot, now.hk * heads));
+            load_tiles(now, now.hk * heads, true);
+        }
         long long place = blockIdx.x;
         for (int n = 0, it = 0; now.ok;) {
             const int hv = now.hk * heads + it, s = now.s, first = now.first, rows = now.rows;
@@ -1184,6 +1189,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             if (2 * lane < rows) p.dg[p.gate.at(s, first + 2 * lane, hv)] = sum;
             if (2 * lane + 1 < rows) p.dg[p.gate.at(s, first + 2 * lane + 1, hv)] = sum - d[0];
             __syncthreads();
+            if (next.ok) load_tiles(next, next_hv, last);
             now = next;
             it = last ? 0 : it + 1;
             n += last;
@@ -1198,7 +1204,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
                 uint32_t w[4];
-                turned_swizzled(tile, quarter * 16, quad * 32 + lh * 16, w);
+                turned(tile, quarter * 16, quad * 32 + lh * 16, w);
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
                     d[i / 4 * 2] = fmaf(x[lh][i], bf16_lo(w[i / 2]), d[i / 4 * 2]);
@@ -1208,24 +1214,17 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             const float sum = token_sum(d, l);
             if ((l.g & 1) == 0) to[quad][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
         };
-        // the tiles and tables of a value head; V for <r, v>, eight tokens a warp and half of the features
+        // V for <r, v>, eight tokens a warp and half of the features
         uint32_t v[8];
         const int row_v = warp % 8 * 8 + l.g;
-        const auto ask = [&](const Unit& x, int hv, bool keys) {
-            if (keys) {
-                copy_tile<kGradThreads>(sm.K, p.K + p.qk.at(x.s, x.first, x.hk), p.qk.token, x.rows, tid);
-                copy_tile<kGradThreads>(sm.Q, p.Q + p.qk.at(x.s, x.first, x.hk), p.qk.token, x.rows, tid);
-            }
-            copy_tile<kGradThreads>(sm.dO, p.dO + p.v.at(x.s, x.first, hv), p.v.token, x.rows, tid);
-            if (tid < kTabs * kC / 4) cp16(sm.tab + tid * 4, chunk_ws(p, x.slot, hv) + kWsTab + tid * 4, true);
-            cp_commit();
+        const auto ask = [&](const Unit& x, int hv) {
             const long long at = p.v.at(x.s, x.first + row_v, hv) + warp / 8 * 64 + 2 * l.c;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = row_v < x.rows ? *reinterpret_cast<const uint32_t*>(p.V + at + i * 8) : 0u;
         };
         float dq[2][8] = {}, dk[2][8] = {};  // [16 lanes][see for_pairs], times 1 / ||q||, 1 / ||k||
         Unit now = units[0];
-        if (now.ok) ask(now, now.hk * heads, true);
+        if (now.ok) ask(now, now.hk * heads);
         uint32_t turn = 0;
         for (int n = 0, it = 0; now.ok; turn ^= 1) {
             const int hv = now.hk * heads + it, s = now.s, first = now.first, rows = now.rows;
@@ -1251,7 +1250,11 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                     }
                 }
             }
-            cp_wait<0>();
+            failed |= !wait_products(&bar_tile, turn);
+            if (rows < kC) {
+                if (it == 0) clear_tail<kGradThreads>(sm.K, rows, tid), clear_tail<kGradThreads>(sm.Q, rows, tid);
+                clear_tail<kGradThreads>(sm.dO, rows, tid);
+            }
             fence_proxy_async_smem();
             grad_arrive<1>();
             grad_sync();
@@ -1388,7 +1391,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             tc_fence_before_sync();
             if (!last) {
                 __syncthreads();
-                ask(now, hv + 1, false);
+                ask(now, hv + 1);
                 ++it;
                 continue;
             }
@@ -1415,7 +1418,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
 #pragma unroll
                 for (int lh = 0; lh < 2; ++lh) {
                     uint32_t w[4];
-                    turned_swizzled(tile, quarter * 16, quad * 32 + lh * 16, w);
+                    turned(tile, quarter * 16, quad * 32 + lh * 16, w);
 #pragma unroll
                     for (int i = 0; i < 8; i += 2)
                         w[i / 2] = pack_bf16x2(fmaf(-c[i / 4 * 2], bf16_lo(w[i / 2]), x[lh][i]), fmaf(-c[i / 4 * 2 + 1], bf16_hi(w[i / 2]), x[lh][i + 1]));
@@ -1429,7 +1432,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             finish(dk, sm.K, sm.tab + TAB_RK * kC, sm.norm[1], out + 2 * kTile);
             __syncthreads();
             const Unit next = units[(n + 1) & 1];
-            if (next.ok) ask(next, next.hk * heads, true);
+            if (next.ok) ask(next, next.hk * heads);
             const long long at = p.qk.at(s, first, now.hk);
 #pragma unroll
             for (int i = tid; i < kC * kD / 8; i += kGradThreads) {
@@ -1452,18 +1455,41 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
     if (warp == 0) tmem_dealloc(tm, kTmColumns);
 }
 
-template <typename Smem>
-bool launch(void (*kern)(ParamsB), long long ctas, unsigned threads, const ParamsB& p, cudaStream_t stream) {
+template <typename Smem, typename... A>
+bool launch(void (*kern)(ParamsB, A...), long long ctas, unsigned threads, cudaStream_t stream, const ParamsB& p, const A&... maps) {
     if (ctas == 0) return true;
     static_assert(sizeof(Smem) + 1024 <= 227 * 1024, "");  // (1 KB to start on a multiple of 1 KB)
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Smem) + 1024) != cudaSuccess) {
         cudaGetLastError();
         return false;
     }
-    kern<<<static_cast<unsigned>(ctas), threads, sizeof(Smem) + 1024, stream>>>(p);
+    kern<<<static_cast<unsigned>(ctas), threads, sizeof(Smem) + 1024, stream>>>(p, maps...);
     if (cudaGetLastError() != cudaSuccess) return false;
     count_launch();
     return true;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn get_encode_fn() {
+    static EncodeTiledFn fn = nullptr;
+    if (fn == nullptr) {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess)
+            return nullptr;
+        fn = reinterpret_cast<EncodeTiledFn>(ptr);
+    }
+    return fn;
+}
+bool make_map(CUtensorMap* map, const void* base, long long planes, int T, int cols) {
+    const EncodeTiledFn enc = get_encode_fn();
+    if (enc == nullptr) return false;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(T), static_cast<cuuint64_t>(planes)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(cols) * 2, static_cast<cuuint64_t>(T) * cols * 2};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(kC), 1}, step[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 long long chunk_places(int n_seq, long long tokens) { return tokens / kC + n_seq; }
@@ -1486,6 +1512,7 @@ int launch_layer_backward(const ProblemB& q, cudaStream_t stream) {
     if (p.status == nullptr) return GDN_ERR_LAUNCH;
     p.scale = q.scale, p.l2norm = (q.flags & GDN_FLAG_K_L2NORM) != 0;
     const bool token_major = (q.flags & GDN_FLAG_LAYOUT_BTHD) != 0, packed = q.cu_seqlens != nullptr;
+    p.token_major = token_major;
     const auto strides = [&](long long H, long long d) {
         Strides s = token_major ? Strides{q.T * H * d, H * d, d} : Strides{q.T * H * d, d, q.T * d};
         if (packed) s.seq = 0;
@@ -1496,10 +1523,18 @@ int launch_layer_backward(const ProblemB& q, cudaStream_t stream) {
     p.units = places * q.H_k;
     const long long chains = static_cast<long long>(q.n_seq) * q.H_v;
     if (places * q.H_k >= (1LL << 31) || chains >= (1LL << 31)) return GDN_ERR_UNSUPPORTED;
-    const bool ok = launch<SmemSystem>(chunk_system_kernel, places * q.H_k, kThreads, p, stream) &&
-                    launch<SmemF>(chunk_states_kernel, chains, kChainThreads, p, stream) &&
-                    launch<SmemB>(chunk_state_grads_kernel, chains, kChainThreads, p, stream) &&
-                    launch<SmemC>(chunk_grads_kernel, p.units < kSMs ? p.units : kSMs, kGradThreads + 32, p, stream);
+    Maps maps{};
+    if (q.T > 0) {
+        const long long batch = packed ? 1 : q.n_seq;
+        const auto map = [&](CUtensorMap* m, const void* base, int H) {
+            return make_map(m, base, token_major ? batch : batch * H, q.T, token_major ? H * kD : kD);
+        };
+        if (!map(&maps.Q, q.Q, q.H_k) || !map(&maps.K, q.K, q.H_k) || !map(&maps.V, q.V, q.H_v) || !map(&maps.dO, q.dO, q.H_v)) return GDN_ERR_LAUNCH;
+    }
+    const bool ok = launch<SmemSystem>(chunk_system_kernel, places * q.H_k, kThreads, stream, p) &&
+                    launch<SmemF>(chunk_states_kernel, chains, kChainThreads, stream, p, maps) &&
+                    launch<SmemB>(chunk_state_grads_kernel, chains, kChainThreads, stream, p, maps) &&
+                    launch<SmemC>(chunk_grads_kernel, p.units < kSMs ? p.units : kSMs, kGradThreads + 32, stream, p, maps);
     return ok ? GDN_OK : GDN_ERR_LAUNCH;
 }
 
