@@ -445,42 +445,35 @@ __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t x)
 // d (128 columns, += if `more`) = A X, A [128 x 64 tokens], X as above
 __device__ __forceinline__ void product_cols(uint32_t d, uint32_t a, uint32_t x, bool more) {
     const uint64_t b = desc_cols(x);
+    constexpr uint32_t idesc = instr_desc(128, 128, 1, 1, 0, 1, 1);
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+    for (int i = kPieces - 1; i >= 0; --i)
 #pragma unroll
-        for (int i = kPieces - 1; i >= 0; --i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                mma_f16_ts(d + half * 64, a + i * 32 + k * 8, b + (half * kTile + k * 2048) / 16, kIdescCols | (i == 1 ? kNegA : 0u),
-                           more || i < kPieces - 1 || k > 0);
+        for (int k = 0; k < 4; ++k)
+            mma_f16_ts(d, a + i * 32 + k * 8, b + k * 2048 / 16, idesc | (i == 1 ? kNegA : 0u), more || i < kPieces - 1 || k > 0);
 }
-// d = A M^T (COLS: A M), both in three pieces, M 64 x 64 and lower triangular in three tiles: the six products of pieces that fp32 can hold, each
-// 16 of the sum at a time and as many columns as those have a part in (from 16 k on; COLS: up to 16 k + 15), the one with all 64 first
-template <bool COLS>
-__device__ __forceinline__ void product_block(uint32_t d, uint32_t a, uint64_t b, int k, bool minus, bool more) {
-    const uint32_t idesc = instr_desc(128, COLS ? 16 * k + 16 : 64 - 16 * k, 1, 1, 0, COLS, 1) | (minus ? kNegA : 0u);
-    mma_f16_ts(COLS ? d : d + 16 * k, a + k * 8, b + (COLS ? k * 2048 : k * (2048 + 32)) / 16, idesc, more);
-}
+// d = A M^T (COLS: A M), both in three pieces, M 64 x 64 in three tiles: the six products of pieces that fp32 can hold. (M is triangular, and
+// products of only the columns that 16 of the sum have a part in would be 62 % of the work; but a change of an instruction's shape costs more.)
 template <bool COLS>
 __device__ __forceinline__ void product_system(uint32_t d, uint32_t a, uint32_t tiles) {
     const uint64_t b = COLS ? desc_cols(tiles) : desc_rows(tiles);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)  // (products of one shape in a row: a change of shape drains the pipe)
+    for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
-        for (int sum = 2; sum >= 0; --sum)
+        for (int i = sum; i >= 0; --i)
 #pragma unroll
-            for (int i = sum; i >= 0; --i) {
-                const int j = sum - i;  // the pieces of A and M; one middle piece: negated
-                product_block<COLS>(d, a + i * 32, b + j * kTile / 16, COLS ? 3 - q : q, (i == 1) != (j == 1), q > 0 || sum < 2 || i < 2);
-            }
+            for (int k = 0; k < 4; ++k)  // pieces i of A and sum - i of M; one middle piece: negated
+                mma_f16_ts(d, a + i * 32 + k * 8, b + ((sum - i) * kTile + k * (COLS ? 2048 : 32)) / 16,
+                           (COLS ? kIdescCols : kIdescRows) | ((i == 1) != (sum - i == 1) ? kNegA : 0u), sum < 2 || i < 2 || k > 0);
 }
-// d = A P, A [128 x 64 tokens] bf16, P lower triangular in three tiles
+// d = A P, A [128 x 64 tokens] bf16, P in three tiles
 __device__ __forceinline__ void product_pairs(uint32_t d, uint32_t a, uint32_t tiles) {
     const uint64_t b = desc_cols(tiles);
 #pragma unroll
-    for (int k = 3; k >= 0; --k)
+    for (int i = kPieces - 1; i >= 0; --i)
 #pragma unroll
-        for (int i = kPieces - 1; i >= 0; --i) product_block<true>(d, a, b + i * kTile / 16, k, i == 1, k < 3 || i < kPieces - 1);
+        for (int k = 0; k < 4; ++k)
+            mma_f16_ts(d, a + k * 8, b + (i * kTile + k * 2048) / 16, kIdescCols | (i == 1 ? kNegA : 0u), i < kPieces - 1 || k > 0);
 }
 
 // a value for each of a thread's 8 x 2 rows and columns: `f(row, column, i)` gets the place of x[i], x[i + 1] (neighbouring columns)
