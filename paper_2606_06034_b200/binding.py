@@ -570,23 +570,24 @@ def gated_delta_layer(Q, K, V, beta, g_raw, C=64, scale=None, S_in=None, *, cu_s
     return O, S_out
 
 
-def _check_tensors(where, device, *tensors):
+def _check_tensors(where, like, *tensors):
     """Contiguous tensors of one CUDA device, the current one (the library launches there)."""
+    device = like.get_device()
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda or t.device != device:
-            raise ValueError(f"{where}: all tensors must live on one CUDA device (there is no CPU path)")
-        if not t.is_contiguous():
+        if t is not None and (t.get_device() != device or not t.is_contiguous()):
+            if not t.is_cuda or t.get_device() != device:
+                raise ValueError(f"{where}: all tensors must live on one CUDA device (there is no CPU path)")
             raise ValueError(f"{where}: all tensors must be contiguous")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"{where}: the tensors live on {device}, which is not the current device")
+    if device < 0:
+        raise ValueError(f"{where}: all tensors must live on one CUDA device (there is no CPU path)")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{where}: the tensors live on {like.device}, which is not the current device")
 
 
 def _check_shape(where, name, t, shape, *dtypes):
     if t is None:
         return
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype not in dtypes:
         raise TypeError(f"{where}: {name} is {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
@@ -629,7 +630,7 @@ def gated_delta_step(Q, K, V, beta, g_raw, S, slots=None, scale=None, *, token_m
     _check_shape(where, "S", S, (S.shape[0], H_v, d_v, d_k), *_TOKEN_TYPES)
     _check_shape(where, "slots", slots, (B,), torch.int32)
     _check_shape(where, "out", out, V.shape, V.dtype)
-    _check_tensors(where, V.device, Q, K, V, beta, g_raw, S, slots, out)
+    _check_tensors(where, V, Q, K, V, beta, g_raw, S, slots, out)
     O = torch.empty_like(V) if out is None else out
     flags = (GDN_FLAG_LAYOUT_BTHD if token_major else 0) | (GDN_FLAG_K_L2NORM if qk_l2norm else 0)
     rc = load_library().gdn_recurrent_step(_ptr(Q), _ptr(K), _ptr(V), _ptr(beta), _ptr(g_raw), B, H_k, H_v, T, d_k, d_v,
@@ -657,7 +658,7 @@ def gated_delta_layer_backward(dO, Q, K, V, beta, g_raw, C=64, scale=None, S_in=
         B = len(bounds) - 1
     for name, t in (("S_in", S_in), ("dS_out", dS_out)):
         _check_shape(where, name, t, (B, H_v, d_v, d_k), torch.float32)
-    _check_tensors(where, V.device, dO, Q, K, V, beta, g_raw, S_in, dS_out, workspace)
+    _check_tensors(where, V, dO, Q, K, V, beta, g_raw, S_in, dS_out, workspace)
     lib = load_library()
     need = int(lib.gdn_gated_delta_layer_backward_workspace(B, T if packed else B * T, H_v))
     if workspace is None:
@@ -686,7 +687,7 @@ def gdn_gated_delta_layer_backward_varlen(dO, Q, K, V, beta, g_raw, cu_seqlens, 
                                           dQ, dK, dV, dbeta, dg, dS_in, workspace, flags, *, check=True):
     """Raw call of the packed form (cu_seqlens: int32 CUDA tensor of n_seq + 1 boundaries); it can be captured in a CUDA graph."""
     tensors = (dO, Q, K, V, beta, g_raw, cu_seqlens, S_in, dS_out, dQ, dK, dV, dbeta, dg, dS_in, workspace)
-    _check_tensors("gdn_gated_delta_layer_backward_varlen", V.device, *tensors)
+    _check_tensors("gdn_gated_delta_layer_backward_varlen", V, *tensors)
     if cu_seqlens is not None and cu_seqlens.dtype != torch.int32:
         raise TypeError("cu_seqlens is an int32 tensor")
     have = 0 if workspace is None else workspace.numel() * workspace.element_size()
@@ -720,7 +721,7 @@ def layer_norm(x, weight=None, bias=None, gate=None, *, rms=False, eps=1e-5, out
     where = "layer_norm"
     rows, width, params = _norm_shapes(where, x, weight, bias, gate)
     _check_shape(where, "out", out, x.shape, x.dtype)
-    _check_tensors(where, x.device, x, weight, bias, gate, out)
+    _check_tensors(where, x, x, weight, bias, gate, out)
     y = torch.empty_like(x) if out is None else out
     rc = load_library().gdn_layer_norm(_ptr(x), _ptr(weight), _ptr(bias), _ptr(gate), rows, width, eps, _dtype_code(x), params, _ptr(y),
                                        GDN_NORM_RMS if rms else 0, _stream())
@@ -735,7 +736,7 @@ def layer_norm_backward(dy, x, weight=None, bias=None, gate=None, *, rms=False, 
     where = "layer_norm_backward"
     rows, width, params = _norm_shapes(where, x, weight, bias, gate)
     _check_shape(where, "dy", dy, x.shape, x.dtype)
-    _check_tensors(where, x.device, dy, x, weight, bias, gate, workspace)
+    _check_tensors(where, x, dy, x, weight, bias, gate, workspace)
     lib = load_library()
     dx = torch.empty_like(x)
     dgate = None if gate is None else torch.empty_like(gate)

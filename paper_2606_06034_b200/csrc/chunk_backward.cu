@@ -38,8 +38,8 @@ constexpr int kC = 64, kD = 128;
 constexpr int kThreads = 256;
 
 // workspace of one chunk of one value head, in floats. T and P: bf16 tiles of three pieces each (see split3); the states: tiles [v][64 keys] of
-// the upper two pieces; all as the products want them in shared memory. u, z, r [v][token]: a feature of the value per row, as the
-// chains have them in tensor memory.
+// the upper two pieces; all as the products want them in shared memory. u, z, r [v][token] fp32: a feature of the value per row, as the
+// chains have them in tensor memory, 16-byte pieces of a row out of order (see vt_at).
 constexpr int kPieces = 3;
 constexpr int kWsT = 0, kWsP = kWsT + kPieces * kC * kC / 2, kWsS = kWsP + kPieces * kC * kC / 2, kWsDS = kWsS + kD * kD, kWsU = kWsDS + kD * kD;
 constexpr int kWsZ = kWsU + kC * kD;     // exp(g) z, then r in its place
@@ -489,6 +489,17 @@ constexpr int kChainThreads = kWorkers + 32 + kLoaders;  // sixteen warps that c
 constexpr int kImage = 2 * 2 * 2 * kTile;     // bytes of a state's tiles: two pieces of two tiles of 128 rows
 // Byte of element (row, col) of a state in its image
 __device__ __forceinline__ int image_at(int piece, int row, int col) { return (piece * 2 + col / 64) * 2 * kTile + swizzled(row, col % 64); }
+// Byte of element (row, token) of u, z or r: 16-byte pieces change places, two by two, with the row's number mod 8: what a warp writes at once (8
+// rows of 8 tokens) lies on all banks
+__device__ __forceinline__ int vt_at(int row, int t) { return row * (kC * 4) + ((((t >> 2) ^ (row << 1)) & 15) << 4) + (t & 3) * 4; }
+// this thread's part of such a matrix
+__device__ __forceinline__ void put_vt(uint8_t* to, const float (&x)[2][8], int row0, int quarter) {
+#pragma unroll
+    for (int lh = 0; lh < 2; ++lh)
+        for_pairs<8>([&](int row, int col, int i) {
+            *reinterpret_cast<float2*>(to + vt_at(row0 + lh * 16 + row, quarter * 16 + col)) = make_float2(x[lh][i], x[lh][i + 1]);
+        });
+}
 // this thread's part of a state (see for_pairs) into the image
 __device__ __forceinline__ void put_image(uint8_t* image, const float (&S)[2][16], int row0, int quarter) {
 #pragma unroll
@@ -562,7 +573,8 @@ struct StageF {  // (the tiles lie on 1 KB)
 };
 struct SmemF {
     StageF stage[2];
-    uint8_t image[kImage];
+    uint8_t image[kImage];  // (u after it)
+    uint8_t z[kD * kC * 4];
 };
 
 __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const ParamsB p, const __grid_constant__ Maps maps) {
@@ -634,6 +646,20 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
                 tma_store_commit();
             }
             __syncwarp();
+            await<4, kLoaders>();
+            if (me == 0) {
+                bulk_store(chunk_ws(p, seq.slot + c, h) + kWsZ, sm.z, sizeof(sm.z));
+                tma_store_commit();
+            }
+            __syncwarp();
+            tma_store_wait_read<1>();  // the image is on its way: u may have its place
+            arrive<5, kLoaders>();
+            await<6, kLoaders>();
+            if (me == 0) {
+                bulk_store(chunk_ws(p, seq.slot + c, h) + kWsU, sm.image, sizeof(sm.z));
+                tma_store_commit();
+            }
+            __syncwarp();
         }
         tma_store_wait_all<0>();
     } else {  // ---- what lies between the products
@@ -649,7 +675,6 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             });
         for (int c = 0; c < n; ++c) {
             const StageF& st = sm.stage[c % 2];
-            float* const ws = chunk_ws(p, seq.slot + c, h);
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) tm_st_split<8>(ch.tm + ch.lanes + (lh << 20) + kTmState + quarter * 16, 64, S[lh]);
             publish();
@@ -677,11 +702,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             }
             publish();
             arrive<1>();
-#pragma unroll
-            for (int lh = 0; lh < 2; ++lh)
-                for_pairs<8>([&](int row, int col, int i) {
-                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + quarter * 16 + col) = make_float2(z[lh][i], z[lh][i + 1]);
-                });
+            put_vt(sm.z, z, row0, quarter);
+            fence_proxy_async_smem();
+            arrive<4, kLoaders>();
             ch.wait();
             float u[2][8];
 #pragma unroll
@@ -697,11 +720,10 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             }
             publish();
             arrive<2>();
-#pragma unroll
-            for (int lh = 0; lh < 2; ++lh)
-                for_pairs<8>([&](int row, int col, int i) {
-                    *reinterpret_cast<float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + quarter * 16 + col) = make_float2(u[lh][i], u[lh][i + 1]);
-                });
+            await<5, kLoaders>();
+            put_vt(sm.image, u, row0, quarter);
+            fence_proxy_async_smem();
+            arrive<6, kLoaders>();
             const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
             ch.wait();
 #pragma unroll
@@ -821,6 +843,8 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             __syncwarp();
             await<6, kLoaders>();  // T and P are used up
             load_system(c - 1);
+            if (c > 0 && me == 0) bulk_prefetch(chunk_ws(p, seq.slot + c - 1, h) + kWsU, 2 * sizeof(float) * kC * kD);
+            __syncwarp();
         }
         tma_store_wait_all<0>();
     } else {  // ---- what lies between the products
@@ -854,7 +878,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
                 for_pairs<8>([&](int row, int col, int i) {
-                    u[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsU + (row0 + lh * 16 + row) * kC + quarter * 16 + col);
+                    u[lh][i / 2] = *reinterpret_cast<const float2*>(reinterpret_cast<const uint8_t*>(ws + kWsU) + vt_at(row0 + lh * 16 + row, quarter * 16 + col));
                 });
             put_image(sm.image, D, row0, quarter);
             fence_proxy_async_smem();
@@ -882,7 +906,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
                 for_pairs<8>([&](int row, int col, int i) {
-                    z[lh][i / 2] = *reinterpret_cast<const float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + quarter * 16 + col);
+                    z[lh][i / 2] = *reinterpret_cast<const float2*>(reinterpret_cast<const uint8_t*>(ws + kWsZ) + vt_at(row0 + lh * 16 + row, quarter * 16 + col));
                 });
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
@@ -916,11 +940,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
             arrive<4>();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh)
-                for_pairs<8>([&](int row, int col, int i) {
+                for_pairs<8>([&](int, int, int i) {
                     dots[0][i / 4 * 2] = fmaf(r[lh][i], z[lh][i / 2].x, dots[0][i / 4 * 2]);
                     dots[0][i / 4 * 2 + 1] = fmaf(r[lh][i + 1], z[lh][i / 2].y, dots[0][i / 4 * 2 + 1]);
-                    *reinterpret_cast<float2*>(ws + kWsZ + (row0 + lh * 16 + row) * kC + quarter * 16 + col) = make_float2(r[lh][i], r[lh][i + 1]);
                 });
+            put_vt(reinterpret_cast<uint8_t*>(ws + kWsZ), r, row0, quarter);
 #pragma unroll
             for (int d = 0; d < kDots; ++d) {
                 const float sum = token_sum(dots[d], l);
@@ -1232,7 +1256,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 grad_sync();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = tid + i * kGradThreads, place = swizzled(at / 16, at % 16 * 4);
+                    const int at = tid + i * kGradThreads, place = swizzled(at / 16, ((at ^ (at / 16 << 1)) & 15) * 4);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         uint32_t w[kPieces][2];

@@ -92,12 +92,26 @@ __device__ __forceinline__ void store8(T* row, int col, int width, bool active, 
             if (active && col + e < width) put(row + col + e, x[e]);
     }
 }
-// 8 elements of weight or bias (fp32 or bf16), `none` where there is no such tensor
+// 8 elements of weight or bias (fp32 or bf16), `none` where there is no such tensor. They are fetched again for every row (from L1), and volatile,
+// so that they do not take registers that rows in flight can use: 128 features, backward, 80 registers instead of 96.
+template <bool VEC>
 __device__ __forceinline__ void load_param(const void* p, bool bf16, int col, int width, float none, float (&x)[8]) {
+    if (p == nullptr || col >= width) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        x[e] = p == nullptr || col + e >= width ? none
-               : bf16 ? one(static_cast<const __nv_bfloat16*>(p) + col + e) : one(static_cast<const float*>(p) + col + e);
+        for (int e = 0; e < 8; ++e) x[e] = none;
+    } else if (VEC && bf16) {
+        Raw8<__nv_bfloat16> r;
+        asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w.x), "=r"(r.w.y), "=r"(r.w.z), "=r"(r.w.w) : "l"(static_cast<const __nv_bfloat16*>(p) + col));
+        r.get(x);
+    } else if (VEC) {
+        const float* const q = static_cast<const float*>(p) + col;
+        asm volatile("ld.global.nc.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "l"(q));
+        asm volatile("ld.global.nc.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(q + 4));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = col + e >= width ? none : bf16 ? one(static_cast<const __nv_bfloat16*>(p) + col + e) : one(static_cast<const float*>(p) + col + e);
+    }
 }
 
 // Sums of two values over the TPR threads of a row. TPR > 32 (the whole CTA): through `box`, of which two calls in a row use
@@ -126,7 +140,7 @@ __device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f +
 
 constexpr int kNormThreads = 256;
 template <int TPR>
-__host__ __device__ constexpr int cta_threads() { return TPR > kNormThreads ? TPR : kNormThreads; }
+__host__ __device__ constexpr int cta_threads() { return TPR > 32 ? TPR : kNormThreads; }
 
 template <typename T, int NV, int TPR>
 __device__ __forceinline__ void statistics(const Raw8<T> (&raw)[NV], int t, const ParamsN& p, float2* box, int& turn, float& mean, float& rstd) {
@@ -158,37 +172,50 @@ __device__ __forceinline__ void statistics(const Raw8<T> (&raw)[NV], int t, cons
     rstd = rsqrtf(q * p.inv_width + p.eps);
 }
 
+// N rows' worth of a tensor's vectors for this thread: those of `row`
+template <typename T, int NV, int TPR, bool VEC>
+__device__ __forceinline__ void load_row(Raw8<T> (&raw)[NV], const void* base, long long row, const ParamsN& p, int t) {
+    const bool active = row < p.rows;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) raw[v] = load8<T, VEC>(static_cast<const T*>(base) + (active ? row : 0) * p.width, (v * TPR + t) * 8, p.width, active);
+}
+
+// A thread asks for its next row before it works on the present one.
 template <typename T, int NV, int TPR, bool VEC>
 __global__ void __launch_bounds__(cta_threads<TPR>()) norm_forward_kernel(const ParamsN p) {
     constexpr int G = cta_threads<TPR>() / TPR;  // rows that a CTA has at a time
     __shared__ float2 box[2 * (TPR > 32 ? TPR / 32 : 1)];
     const int t = threadIdx.x % TPR;
+    const long long step = static_cast<long long>(gridDim.x) * G;
     int turn = 0;
-    float w[NV][8], b[NV][8];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        load_param(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w[v]);
-        load_param(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, b[v]);
-    }
-    for (long long first = static_cast<long long>(blockIdx.x) * G; first < p.rows; first += static_cast<long long>(gridDim.x) * G) {
-        const long long row = first + threadIdx.x / TPR;
+    Raw8<T> next[NV], next_gate[NV];
+    long long row = static_cast<long long>(blockIdx.x) * G + threadIdx.x / TPR;
+    load_row<T, NV, TPR, VEC>(next, p.x, row, p, t);
+    if (p.gate != nullptr) load_row<T, NV, TPR, VEC>(next_gate, p.gate, row, p, t);
+    for (long long first = static_cast<long long>(blockIdx.x) * G; first < p.rows; first += step, row += step) {
         const bool active = row < p.rows;
         const long long at = (active ? row : 0) * p.width;
         Raw8<T> raw[NV], gate[NV];
 #pragma unroll
-        for (int v = 0; v < NV; ++v) raw[v] = load8<T, VEC>(static_cast<const T*>(p.x) + at, (v * TPR + t) * 8, p.width, active);
-        if (p.gate != nullptr) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) gate[v] = load8<T, VEC>(static_cast<const T*>(p.gate) + at, (v * TPR + t) * 8, p.width, active);
+        for (int v = 0; v < NV; ++v) raw[v] = next[v], gate[v] = next_gate[v];
+        if (first + step < p.rows) {
+            load_row<T, NV, TPR, VEC>(next, p.x, row + step, p, t);
+            if (p.gate != nullptr) load_row<T, NV, TPR, VEC>(next_gate, p.gate, row + step, p, t);
         }
         float mean, rstd;
         statistics<T, NV, TPR>(raw, t, p, box, turn, mean, rstd);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float x[8], z[8];
+            float x[8], z[8], w[8];
             raw[v].get(x);
+            load_param<VEC>(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = fmaf((x[e] - mean) * rstd, w[v][e], b[v][e]);
+            for (int e = 0; e < 8; ++e) x[e] = (x[e] - mean) * rstd * w[e];
+            if (p.bias != nullptr) {
+                load_param<VEC>(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += w[e];
+            }
             if (p.gate != nullptr) {
                 gate[v].get(z);
 #pragma unroll
@@ -200,48 +227,48 @@ __global__ void __launch_bounds__(cta_threads<TPR>()) norm_forward_kernel(const 
 }
 
 template <typename T, int NV, int TPR, bool VEC>
-__global__ void __launch_bounds__(cta_threads<TPR>()) norm_backward_kernel(const ParamsN p) {
+__global__ void __launch_bounds__(cta_threads<TPR>(), NV == 1 && sizeof(T) == 2 ? 768 / cta_threads<TPR>() : 1) norm_backward_kernel(const ParamsN p) {
     constexpr int G = cta_threads<TPR>() / TPR;
     constexpr int kColumns = NV * TPR * 8;
     __shared__ float2 box[2 * (TPR > 32 ? TPR / 32 : 1)];
     __shared__ float gather[G > 1 ? G * kColumns : 1];
     const int t = threadIdx.x % TPR;
     int turn = 0;
-    float w[NV][8], b[NV][8], dw[NV][8] = {}, db[NV][8] = {};
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        load_param(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w[v]);
-        load_param(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, b[v]);
-    }
-    for (long long first = static_cast<long long>(blockIdx.x) * G; first < p.rows; first += static_cast<long long>(gridDim.x) * G) {
-        const long long row = first + threadIdx.x / TPR;
+    float dw[NV][8] = {}, db[NV][8] = {};
+    const long long step = static_cast<long long>(gridDim.x) * G;
+    Raw8<T> next[NV], next_gate[NV], next_up[NV];
+    long long row = static_cast<long long>(blockIdx.x) * G + threadIdx.x / TPR;
+    const auto ask = [&](long long r) {
+        load_row<T, NV, TPR, VEC>(next, p.x, r, p, t);
+        load_row<T, NV, TPR, VEC>(next_up, p.dy, r, p, t);
+        if (p.gate != nullptr) load_row<T, NV, TPR, VEC>(next_gate, p.gate, r, p, t);
+    };
+    ask(row);
+    for (long long first = static_cast<long long>(blockIdx.x) * G; first < p.rows; first += step, row += step) {
         const bool active = row < p.rows;
         const long long at = (active ? row : 0) * p.width;
         Raw8<T> raw[NV], gate[NV], up[NV];
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            raw[v] = load8<T, VEC>(static_cast<const T*>(p.x) + at, (v * TPR + t) * 8, p.width, active);
-            up[v] = load8<T, VEC>(static_cast<const T*>(p.dy) + at, (v * TPR + t) * 8, p.width, active);
-        }
-        if (p.gate != nullptr) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) gate[v] = load8<T, VEC>(static_cast<const T*>(p.gate) + at, (v * TPR + t) * 8, p.width, active);
-        }
+        for (int v = 0; v < NV; ++v) raw[v] = next[v], gate[v] = next_gate[v], up[v] = next_up[v];
+        if (first + step < p.rows) ask(row + step);
         float mean, rstd;
         statistics<T, NV, TPR>(raw, t, p, box, turn, mean, rstd);
         // dh, its sums, the gate's gradient. Elements past the width have dy = 0 and so count for nothing.
         float dh[NV][8], c0 = 0.f, c1 = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float x[8], z[8], dz[8];
+            float x[8], w[8];
             raw[v].get(x);
             up[v].get(dh[v]);
+            load_param<VEC>(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w);
             if (p.gate != nullptr) {
+                float z[8], dz[8], b[8];
                 gate[v].get(z);
+                load_param<VEC>(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, b);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float s = sigmoid(z[e]), n = (x[e] - mean) * rstd;
-                    dz[e] = dh[v][e] * fmaf(n, w[v][e], b[v][e]) * s * fmaf(z[e], 1.f - s, 1.f);
+                    dz[e] = dh[v][e] * fmaf(n, w[e], b[e]) * s * fmaf(z[e], 1.f - s, 1.f);
                     dh[v][e] *= z[e] * s;
                 }
                 store8<T, VEC>(static_cast<T*>(p.dgate) + at, (v * TPR + t) * 8, p.width, active, dz);
@@ -253,7 +280,7 @@ __global__ void __launch_bounds__(cta_threads<TPR>()) norm_backward_kernel(const
                     dw[v][e] = fmaf(dh[v][e], n, dw[v][e]);
                     db[v][e] += dh[v][e];
                 }
-                dh[v][e] *= w[v][e];
+                dh[v][e] *= w[e];
                 c0 += dh[v][e];
                 c1 = fmaf(dh[v][e], n, c1);
             }
@@ -320,21 +347,20 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, in
     }
 }
 
-constexpr int kForwardPerSM = 8, kBackwardPerSM = 4;  // CTAs of 256 threads that a launch brings, at most
+constexpr int kForwardThreads = 2048, kBackwardThreads = 1024;  // threads that a launch brings per SM, at most
 
-// threads of a row, and rows that a CTA has at a time
-int row_threads(int width) { return width <= 128 ? 16 : width <= 1024 ? 32 : width <= 8192 ? 256 : 512; }
+// threads of a row; CTAs of a launch
+int row_threads(int width) { return width <= 128 ? 16 : width <= 512 ? 32 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512; }
 long long cta_count(long long rows, int width, int per_sm) {
-    const int tpr = row_threads(width);
-    const int g = tpr > kNormThreads ? 1 : kNormThreads / tpr;
-    const long long need = (rows + g - 1) / g, most = static_cast<long long>(per_sm) * kSMs;
+    const int tpr = row_threads(width), threads = tpr > 32 ? tpr : kNormThreads, g = threads / tpr;
+    const long long need = (rows + g - 1) / g, most = static_cast<long long>(per_sm / threads) * kSMs;
     return need < most ? need : most;
 }
 
 template <typename T, int NV, int TPR>
 int launch_norm(const ParamsN& p, bool backward, cudaStream_t stream) {
     const bool vec = p.width % 8 == 0;
-    const unsigned grid = static_cast<unsigned>(cta_count(p.rows, p.width, backward ? kBackwardPerSM : kForwardPerSM));
+    const unsigned grid = static_cast<unsigned>(cta_count(p.rows, p.width, backward ? kBackwardThreads : kForwardThreads));
     if (grid > 0) {
         auto* kern = backward ? (vec ? norm_backward_kernel<T, NV, TPR, true> : norm_backward_kernel<T, NV, TPR, false>)
                               : (vec ? norm_forward_kernel<T, NV, TPR, true> : norm_forward_kernel<T, NV, TPR, false>);
@@ -351,17 +377,17 @@ int launch_norm_width(const ParamsN& p, bool backward, cudaStream_t stream) {
     if (w <= 128) return launch_norm<T, 1, 16>(p, backward, stream);
     if (w <= 256) return launch_norm<T, 1, 32>(p, backward, stream);
     if (w <= 512) return launch_norm<T, 2, 32>(p, backward, stream);
-    if (w <= 1024) return launch_norm<T, 4, 32>(p, backward, stream);
+    if (w <= 1024) return launch_norm<T, 1, 128>(p, backward, stream);
     if (w <= 2048) return launch_norm<T, 1, 256>(p, backward, stream);
-    if (w <= 4096) return launch_norm<T, 2, 256>(p, backward, stream);
-    if (w <= 8192) return launch_norm<T, 4, 256>(p, backward, stream);
+    if (w <= 4096) return launch_norm<T, 1, 512>(p, backward, stream);
+    if (w <= 8192) return launch_norm<T, 2, 512>(p, backward, stream);
     return launch_norm<T, 4, 512>(p, backward, stream);
 }
 
 }  // namespace
 
 size_t norm_workspace(long long rows, int width) {
-    return static_cast<size_t>(cta_count(rows, width, kBackwardPerSM)) * 2 * width * sizeof(float);
+    return static_cast<size_t>(cta_count(rows, width, kBackwardThreads)) * 2 * width * sizeof(float);
 }
 
 int launch_layer_norm(const ProblemN& q, bool backward, cudaStream_t stream) {
@@ -374,7 +400,7 @@ int launch_layer_norm(const ProblemN& q, bool backward, cudaStream_t stream) {
     p.partial = backward && (q.dweight != nullptr || q.dbias != nullptr) ? static_cast<float*>(q.workspace) : nullptr;
     const int rc = q.dtype == GDN_DTYPE_BF16 ? launch_norm_width<__nv_bfloat16>(p, backward, stream) : launch_norm_width<float>(p, backward, stream);
     if (rc != GDN_OK || p.partial == nullptr) return rc;
-    const int parts = static_cast<int>(cta_count(q.rows, q.width, kBackwardPerSM));
+    const int parts = static_cast<int>(cta_count(q.rows, q.width, kBackwardThreads));
     float *const dw = q.dweight, *const db = q.dbias;
     const dim3 grid((q.width + 31) / 32, db != nullptr ? 2 : 1);  // (without a weight there may be a bias)
     cudaLaunchAttribute attr{};
