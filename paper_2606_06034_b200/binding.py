@@ -178,8 +178,14 @@ def _ptr(t):
     return t.data_ptr()  # (the argument types turn it into a pointer)
 
 
+# The handle of torch's current stream without the stream object around it, which costs 5 us a call (a short call is 10 us in all)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _int32_table(values, device):
@@ -599,22 +605,27 @@ _TOKEN_TYPES = (torch.bfloat16, torch.float32)
 def _layer_shapes(where, Q, K, V, beta, g, token_major, packed, *dtypes):
     """Sizes (B, H_k, H_v, T, d_k, d_v) of a layer's tensors, after a check that they fit each other."""
     dims = 3 if packed else 4
-    if V.dim() != dims or K.dim() != dims:
+    key, val = K.shape, V.shape
+    if len(key) != dims or len(val) != dims:
         raise ValueError(f"{where}: Q, K, V have {dims} dimensions here")
     if token_major:
-        lead, (H_k, d_k), (H_v, d_v) = tuple(V.shape[:-2]), K.shape[-2:], V.shape[-2:]
-        T = lead[-1]
-        key, val, gate = (*lead, H_k, d_k), (*lead, H_v, d_v), (*lead, H_v)
+        T, H_k, d_k = key[-3:]
+        H_v, d_v = val[-2:]
+        lead, gate = key[:-2] == val[:-2], val[:-1]
     else:
-        lead, (H_k, T, d_k), (H_v, _, d_v) = tuple(V.shape[:-3]), K.shape[-3:], V.shape[-3:]
-        key, val, gate = (*lead, H_k, T, d_k), (*lead, H_v, T, d_v), (*lead, H_v, T)
-    for name, t, shape in (("Q", Q, key), ("K", K, key), ("V", V, val)):
-        _check_shape(where, name, t, shape, *dtypes)
-    if not Q.dtype == K.dtype == V.dtype:
-        raise TypeError(f"{where}: Q, K and V share a dtype")
-    for name, t in (("beta", beta), ("g_raw", g)):
-        _check_shape(where, name, t, gate, torch.float32)
-    return (1 if packed else V.shape[0]), H_k, H_v, T, d_k, d_v
+        H_k, T, d_k = key[-3:]
+        H_v, d_v = val[-3], val[-1]
+        lead, gate = key[:-3] == val[:-3] and val[-2] == T, val[:-1]
+    dtype = V.dtype
+    if Q.shape != key or not lead:
+        raise ValueError(f"{where}: Q {tuple(Q.shape)}, K {tuple(key)} and V {tuple(val)} do not belong together")
+    if dtype not in dtypes or Q.dtype != dtype or K.dtype != dtype:
+        raise TypeError(f"{where}: Q, K and V share a dtype, {' or '.join(str(d) for d in dtypes)}")
+    if beta.shape != gate or g.shape != gate:
+        raise ValueError(f"{where}: beta {tuple(beta.shape)} and g_raw {tuple(g.shape)}, expected {tuple(gate)}")
+    if beta.dtype != torch.float32 or g.dtype != torch.float32:
+        raise TypeError(f"{where}: beta and g_raw are fp32")
+    return (1 if packed else val[0]), H_k, H_v, T, d_k, d_v
 
 
 def gated_delta_step(Q, K, V, beta, g_raw, S, slots=None, scale=None, *, token_major=True, qk_l2norm=True, out=None):

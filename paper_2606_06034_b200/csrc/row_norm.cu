@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, in
     if (out == nullptr) return;
     float s = 0.f;
     if (col < width)
-#pragma unroll 4
+#pragma unroll 8
         for (int i = threadIdx.y; i < parts; i += 32) s += partial[(static_cast<long long>(i) * 2 + blockIdx.y) * width + col];
     box[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
