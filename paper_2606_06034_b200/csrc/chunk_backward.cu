@@ -183,13 +183,15 @@ struct SmemSystem {
         struct {
             __nv_bfloat16 K[kC * kLdX], Q[kC * kLdX];
         } in;
-        float T[kC * kLdV];
+        struct {
+            float T[kC * kLdV], A[kC * kLdV];
+        };
     };
-    float kk[kC * kLdV], qk[kC * kLdV], A[kC * kLdV];
+    float kk[kC * kLdV], qk[kC * kLdV];
     float rk[kC], rq[kC], g[kC], beta[kC];
 };
 
-__global__ void __launch_bounds__(kThreads) chunk_system_kernel(const ParamsB p) {
+__global__ void __launch_bounds__(kThreads, 3) chunk_system_kernel(const ParamsB p) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SmemSystem& sm = *reinterpret_cast<SmemSystem*>(smem_raw);
     const int hk = blockIdx.x % p.H_k, slot = blockIdx.x / p.H_k;
@@ -287,24 +289,50 @@ __global__ void __launch_bounds__(kThreads) chunk_system_kernel(const ParamsB p)
             store_pieces(ws + kWsP, row, col, q);
         }
         __syncthreads();
-        {  // column j of T by forward substitution: x_i = [i = j] - sum_k A_ik x_k, four threads a column
-            const int j = tid / 4, part = tid % 4;
-            float x[16];
+        // T = (I + A)^-1: the two diagonal blocks of 32 by forward substitution, column j of either x_i = [i = j] - sum_k A_ik x_k, four
+        // threads a column; the block below them is -T22 A21 T11. (By substitution alone the kernel, which shared memory bounds, takes 0.77 ms
+        // for 16384 chunks, so 0.61.)
+        {
+            const int j = tid / 4, part = tid % 4, r0 = j & 32;
+            float x[8];
 #pragma unroll
-            for (int m = 0; m < 16; ++m) x[m] = 0.f;
+            for (int m = 0; m < 8; ++m) x[m] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kC; ++i) {
+            for (int i = 0; i < 32; ++i) {
                 float a = 0.f, b = 0.f;
 #pragma unroll
                 for (int m = 0; m <= i / 4; m += 2) {
-                    a = fmaf(sm.A[i * kLdV + 4 * m + part], x[m], a);
-                    if (m + 1 <= i / 4) b = fmaf(sm.A[i * kLdV + 4 * m + 4 + part], x[m + 1], b);
+                    a = fmaf(sm.A[(r0 + i) * kLdV + r0 + 4 * m + part], x[m], a);
+                    if (m + 1 <= i / 4) b = fmaf(sm.A[(r0 + i) * kLdV + r0 + 4 * m + 4 + part], x[m + 1], b);
                 }
-                const float xi = (i == j ? 1.f : 0.f) - quad_sum(a + b);
+                const float xi = (r0 + i == j ? 1.f : 0.f) - quad_sum(a + b);
                 if (i % 4 == part) x[i / 4] = xi;
             }
 #pragma unroll
-            for (int m = 0; m < 16; ++m) sm.T[(4 * m + part) * kLdV + j] = x[m];
+            for (int m = 0; m < 8; ++m) sm.T[(r0 + 4 * m + part) * kLdV + j] = x[m];
+        }
+        __syncthreads();
+        {
+            const int i = tid / 8, c = tid % 8 * 4;
+            const auto product = [&](const float* row, const float* m) {  // row [32] times m [32][4]
+                float4 d = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                    const float4 r = *reinterpret_cast<const float4*>(row + k);
+                    const float w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 v = *reinterpret_cast<const float4*>(m + (k + e) * kLdV);
+                        d.x = fmaf(w[e], v.x, d.x), d.y = fmaf(w[e], v.y, d.y), d.z = fmaf(w[e], v.z, d.z), d.w = fmaf(w[e], v.w, d.w);
+                    }
+                }
+                return d;
+            };
+            *reinterpret_cast<float4*>(sm.A + i * kLdV + 32 + c) = product(sm.A + (32 + i) * kLdV, sm.T + c);  // (A has nothing above its diagonal)
+            *reinterpret_cast<float4*>(sm.T + i * kLdV + 32 + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+            __syncthreads();
+            const float4 d = product(sm.T + (32 + i) * kLdV + 32, sm.A + 32 + c);
+            *reinterpret_cast<float4*>(sm.T + (32 + i) * kLdV + c) = make_float4(-d.x, -d.y, -d.z, -d.w);
         }
         __syncthreads();
         for (int i = tid; i < kC * kC / 4; i += kThreads) {
