@@ -29,30 +29,38 @@ struct ParamsN {
     bool rms, param_bf16, want_db;
 };
 
-// 8 elements of a row, as they are stored
+// 8 elements of a row, as they are stored. They are worked on as four packed pairs: the arithmetic is what bounds the kernels beside the HBM.
 template <typename T>
 struct Raw8;
 template <>
 struct Raw8<__nv_bfloat16> {
     uint4 w;
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        x[0] = bf16_lo(w.x), x[1] = bf16_hi(w.x), x[2] = bf16_lo(w.y), x[3] = bf16_hi(w.y);
-        x[4] = bf16_lo(w.z), x[5] = bf16_hi(w.z), x[6] = bf16_lo(w.w), x[7] = bf16_hi(w.w);
+    __device__ __forceinline__ void get(f2 (&x)[4]) const {
+        x[0] = pair2(bf16_lo(w.x), bf16_hi(w.x)), x[1] = pair2(bf16_lo(w.y), bf16_hi(w.y));
+        x[2] = pair2(bf16_lo(w.z), bf16_hi(w.z)), x[3] = pair2(bf16_lo(w.w), bf16_hi(w.w));
     }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
-        w = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+    __device__ __forceinline__ void set(const f2 (&x)[4]) {
+        float a[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpair2(x[i], a[2 * i], a[2 * i + 1]);
+        w = make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7]));
     }
 };
 template <>
 struct Raw8<float> {
     float4 a, b;
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
-        a = make_float4(x[0], x[1], x[2], x[3]), b = make_float4(x[4], x[5], x[6], x[7]);
+    __device__ __forceinline__ void get(f2 (&x)[4]) const { x[0] = pair2(a.x, a.y), x[1] = pair2(a.z, a.w), x[2] = pair2(b.x, b.y), x[3] = pair2(b.z, b.w); }
+    __device__ __forceinline__ void set(const f2 (&x)[4]) {
+        unpair2(x[0], a.x, a.y), unpair2(x[1], a.z, a.w);
+        unpair2(x[2], b.x, b.y), unpair2(x[3], b.z, b.w);
     }
 };
+__device__ __forceinline__ f2 both(float x) { return pair2(x, x); }
+__device__ __forceinline__ float sum2(f2 x) {
+    float a, b;
+    unpair2(x, a, b);
+    return a + b;
+}
 __device__ __forceinline__ float one(const float* p) { return *p; }
 __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
@@ -63,23 +71,19 @@ __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bf
 template <typename T, bool VEC>
 __device__ __forceinline__ Raw8<T> load8(const T* row, int col, int width, bool active) {
     Raw8<T> r;
-    if (VEC) {
-        if (active && col < width) {
-            r = *reinterpret_cast<const Raw8<T>*>(row + col);
-        } else {
-            const float zero[8] = {};
-            r.set(zero);
-        }
+    if (VEC && active && col < width) {
+        r = *reinterpret_cast<const Raw8<T>*>(row + col);
     } else {
-        float x[8];
+        f2 x[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = active && col + e < width ? one(row + col + e) : 0.f;
+        for (int i = 0; i < 4; ++i)
+            x[i] = VEC ? both(0.f) : pair2(active && col + 2 * i < width ? one(row + col + 2 * i) : 0.f, active && col + 2 * i + 1 < width ? one(row + col + 2 * i + 1) : 0.f);
         r.set(x);
     }
     return r;
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* row, int col, int width, bool active, const float (&x)[8]) {
+__device__ __forceinline__ void store8(T* row, int col, int width, bool active, const f2 (&x)[4]) {
     if (VEC) {
         if (active && col < width) {
             Raw8<T> r;
@@ -88,88 +92,105 @@ __device__ __forceinline__ void store8(T* row, int col, int width, bool active, 
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (active && col + e < width) put(row + col + e, x[e]);
+        for (int i = 0; i < 4; ++i) {
+            float a, b;
+            unpair2(x[i], a, b);
+            if (active && col + 2 * i < width) put(row + col + 2 * i, a);
+            if (active && col + 2 * i + 1 < width) put(row + col + 2 * i + 1, b);
+        }
     }
 }
 // 8 elements of weight or bias (fp32 or bf16), `none` where there is no such tensor. They are fetched again for every row (from L1), and volatile,
 // so that they do not take registers that rows in flight can use: 128 features, backward, 80 registers instead of 96.
 template <bool VEC>
-__device__ __forceinline__ void load_param(const void* p, bool bf16, int col, int width, float none, float (&x)[8]) {
+__device__ __forceinline__ void load_param(const void* p, bool bf16, int col, int width, float none, f2 (&x)[4]) {
     if (p == nullptr || col >= width) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = none;
+        for (int i = 0; i < 4; ++i) x[i] = both(none);
     } else if (VEC && bf16) {
         Raw8<__nv_bfloat16> r;
         asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w.x), "=r"(r.w.y), "=r"(r.w.z), "=r"(r.w.w) : "l"(static_cast<const __nv_bfloat16*>(p) + col));
         r.get(x);
     } else if (VEC) {
         const float* const q = static_cast<const float*>(p) + col;
-        asm volatile("ld.global.nc.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "l"(q));
-        asm volatile("ld.global.nc.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(q + 4));
+        asm volatile("ld.global.nc.v2.u64 {%0,%1}, [%2];" : "=l"(x[0]), "=l"(x[1]) : "l"(q));
+        asm volatile("ld.global.nc.v2.u64 {%0,%1}, [%2];" : "=l"(x[2]), "=l"(x[3]) : "l"(q + 4));
     } else {
+        const auto at = [&](int c) { return c >= width ? none : bf16 ? one(static_cast<const __nv_bfloat16*>(p) + c) : one(static_cast<const float*>(p) + c); };
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            x[e] = col + e >= width ? none : bf16 ? one(static_cast<const __nv_bfloat16*>(p) + col + e) : one(static_cast<const float*>(p) + col + e);
+        for (int i = 0; i < 4; ++i) x[i] = pair2(at(col + 2 * i), at(col + 2 * i + 1));
     }
 }
 
-// Sums of two values over the TPR threads of a row. TPR > 32 (the whole CTA): through `box`, of which two calls in a row use
+// Sums of N values over the TPR threads of a row. TPR > 32 (the whole CTA): through `box`, of which two calls in a row use
 // different halves, so that one barrier a call is enough.
-template <int TPR>
-__device__ __forceinline__ void row_sums(float& a, float& b, float2* box, int& turn) {
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&x)[N], float2* box, int& turn) {
 #pragma unroll
-    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
-        a += __shfl_xor_sync(0xffffffffu, a, o);
-        b += __shfl_xor_sync(0xffffffffu, b, o);
-    }
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
     if (TPR > 32) {
         constexpr int W = TPR / 32;
         float2* const half = box + turn * W;
         turn ^= 1;
-        if (threadIdx.x % 32 == 0) half[threadIdx.x / 32] = make_float2(a, b);
+        if (threadIdx.x % 32 == 0) half[threadIdx.x / 32] = make_float2(x[0], x[N - 1]);
         __syncthreads();
-        a = b = 0.f;
+        f2 s = both(0.f);
 #pragma unroll
-        for (int i = 0; i < W; ++i) a += half[i].x, b += half[i].y;
+        for (int i = 0; i < W; ++i) s = add2(s, *reinterpret_cast<const f2*>(half + i));
+        float a, b;
+        unpair2(s, a, b);
+        x[0] = a;
+        if (N == 2) x[N - 1] = b;
     }
 }
 
 // sigmoid; exp(-z) = inf gives 0
 __device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ f2 sigmoid(f2 z) {
+    float a, b;
+    unpair2(z, a, b);
+    return pair2(sigmoid(a), sigmoid(b));
+}
 
 constexpr int kNormThreads = 256;
 template <int TPR>
 __host__ __device__ constexpr int cta_threads() { return TPR > 32 ? TPR : kNormThreads; }
 
-template <typename T, int NV, int TPR>
-__device__ __forceinline__ void statistics(const Raw8<T> (&raw)[NV], int t, const ParamsN& p, float2* box, int& turn, float& mean, float& rstd) {
-    float s = 0.f, unused = 0.f;
-    mean = 0.f;
+// The row's values less their mean (past the width: zeros), and one over their deviation
+template <typename T, int NV, int TPR, bool VEC>
+__device__ __forceinline__ float centred(const Raw8<T> (&raw)[NV], f2 (&x)[NV][4], int t, const ParamsN& p, float2* box, int& turn) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int v = 0; v < NV; ++v) raw[v].get(x[v]);
     if (!p.rms) {
 #pragma unroll
+        for (int v = 0; v < NV; ++v) s[0] += sum2(add2(add2(x[v][0], x[v][1]), add2(x[v][2], x[v][3])));
+        row_sums<TPR>(s, box, turn);
+        const float mean = s[0] * p.inv_width;
+#pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float x[8];
-            raw[v].get(x);
+            const int col = (v * TPR + t) * 8;
+            if (VEC) {
+                if (col < p.width) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += x[e];
-        }
-        row_sums<TPR>(s, unused, box, turn);
-        mean = s * p.inv_width;
-    }
-    float q = 0.f;
+                    for (int i = 0; i < 4; ++i) x[v][i] = add2(x[v][i], both(-mean));
+                }
+            } else {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        float x[8];
-        raw[v].get(x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float d = (v * TPR + t) * 8 + e < p.width ? x[e] - mean : 0.f;
-            q = fmaf(d, d, q);
+                for (int i = 0; i < 4; ++i) x[v][i] = add2(x[v][i], pair2(col + 2 * i < p.width ? -mean : 0.f, col + 2 * i + 1 < p.width ? -mean : 0.f));
+            }
         }
     }
-    row_sums<TPR>(q, unused, box, turn);
-    rstd = rsqrtf(q * p.inv_width + p.eps);
+    f2 q = both(0.f);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q = fma2(x[v][i], x[v][i], q);
+    s[0] = sum2(q);
+    row_sums<TPR>(s, box, turn);
+    return rsqrtf(s[0] * p.inv_width + p.eps);
 }
 
 // N rows' worth of a tensor's vectors for this thread: those of `row`
@@ -202,26 +223,26 @@ __global__ void __launch_bounds__(cta_threads<TPR>()) norm_forward_kernel(const 
             load_row<T, NV, TPR, VEC>(next, p.x, row + step, p, t);
             if (p.gate != nullptr) load_row<T, NV, TPR, VEC>(next_gate, p.gate, row + step, p, t);
         }
-        float mean, rstd;
-        statistics<T, NV, TPR>(raw, t, p, box, turn, mean, rstd);
+        f2 x[NV][4];
+        const f2 rstd = both(centred<T, NV, TPR, VEC>(raw, x, t, p, box, turn));
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float x[8], z[8], w[8];
-            raw[v].get(x);
+            f2 w[4];
             load_param<VEC>(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (x[e] - mean) * rstd * w[e];
+            for (int i = 0; i < 4; ++i) x[v][i] = mul2(mul2(x[v][i], rstd), w[i]);
             if (p.bias != nullptr) {
                 load_param<VEC>(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] += w[e];
+                for (int i = 0; i < 4; ++i) x[v][i] = add2(x[v][i], w[i]);
             }
             if (p.gate != nullptr) {
+                f2 z[4];
                 gate[v].get(z);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= z[e] * sigmoid(z[e]);
+                for (int i = 0; i < 4; ++i) x[v][i] = mul2(x[v][i], mul2(z[i], sigmoid(z[i])));
             }
-            store8<T, VEC>(static_cast<T*>(p.y) + at, (v * TPR + t) * 8, p.width, active, x);
+            store8<T, VEC>(static_cast<T*>(p.y) + at, (v * TPR + t) * 8, p.width, active, x[v]);
         }
     }
 }
@@ -234,7 +255,11 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), NV == 1 && sizeof(T) == 2 
     __shared__ float gather[G > 1 ? G * kColumns : 1];
     const int t = threadIdx.x % TPR;
     int turn = 0;
-    float dw[NV][8] = {}, db[NV][8] = {};
+    f2 dw[NV][4], db[NV][4];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dw[v][i] = db[v][i] = both(0.f);
     const long long step = static_cast<long long>(gridDim.x) * G;
     Raw8<T> next[NV], next_gate[NV], next_up[NV];
     long long row = static_cast<long long>(blockIdx.x) * G + threadIdx.x / TPR;
@@ -251,50 +276,48 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), NV == 1 && sizeof(T) == 2 
 #pragma unroll
         for (int v = 0; v < NV; ++v) raw[v] = next[v], gate[v] = next_gate[v], up[v] = next_up[v];
         if (first + step < p.rows) ask(row + step);
-        float mean, rstd;
-        statistics<T, NV, TPR>(raw, t, p, box, turn, mean, rstd);
-        // dh, its sums, the gate's gradient. Elements past the width have dy = 0 and so count for nothing.
-        float dh[NV][8], c0 = 0.f, c1 = 0.f;
+        f2 n[NV][4], dh[NV][4];
+        const float rstd = centred<T, NV, TPR, VEC>(raw, n, t, p, box, turn);
+        // dh, its sums, the gate's gradient. Elements past the width, and rows past the last, have dy = 0 and n = 0 and so count for nothing.
+        f2 c0 = both(0.f), c1 = both(0.f);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float x[8], w[8];
-            raw[v].get(x);
+            f2 w[4];
             up[v].get(dh[v]);
             load_param<VEC>(p.weight, p.param_bf16, (v * TPR + t) * 8, p.width, 1.f, w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n[v][i] = mul2(n[v][i], both(rstd));
             if (p.gate != nullptr) {
-                float z[8], dz[8], b[8];
+                f2 z[4], b[4];
                 gate[v].get(z);
                 load_param<VEC>(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, b);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float s = sigmoid(z[e]), n = (x[e] - mean) * rstd;
-                    dz[e] = dh[v][e] * fmaf(n, w[e], b[e]) * s * fmaf(z[e], 1.f - s, 1.f);
-                    dh[v][e] *= z[e] * s;
+                for (int i = 0; i < 4; ++i) {
+                    const f2 s = sigmoid(z[i]), zs = mul2(z[i], s);
+                    // silu'(z) = s + z s (1 - s)
+                    const f2 slope = fma2(zs, fma2(s, both(-1.f), both(1.f)), s), h = fma2(n[v][i], w[i], b[i]);
+                    z[i] = mul2(mul2(dh[v][i], h), slope);
+                    dh[v][i] = mul2(dh[v][i], zs);
                 }
-                store8<T, VEC>(static_cast<T*>(p.dgate) + at, (v * TPR + t) * 8, p.width, active, dz);
+                store8<T, VEC>(static_cast<T*>(p.dgate) + at, (v * TPR + t) * 8, p.width, active, z);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float n = (x[e] - mean) * rstd;
-                if (active) {
-                    dw[v][e] = fmaf(dh[v][e], n, dw[v][e]);
-                    db[v][e] += dh[v][e];
-                }
-                dh[v][e] *= w[e];
-                c0 += dh[v][e];
-                c1 = fmaf(dh[v][e], n, c1);
+            for (int i = 0; i < 4; ++i) {
+                dw[v][i] = fma2(dh[v][i], n[v][i], dw[v][i]);
+                db[v][i] = add2(db[v][i], dh[v][i]);
+                dh[v][i] = mul2(dh[v][i], w[i]);
+                c0 = add2(c0, dh[v][i]);
+                c1 = fma2(dh[v][i], n[v][i], c1);
             }
         }
-        row_sums<TPR>(c0, c1, box, turn);
-        c0 = p.rms ? 0.f : c0 * p.inv_width;
-        c1 *= p.inv_width;
+        float c[2] = {sum2(c0), sum2(c1)};
+        row_sums<TPR>(c, box, turn);
+        const f2 m0 = both(p.rms ? 0.f : -c[0] * p.inv_width), m1 = both(-c[1] * p.inv_width);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float x[8];
-            raw[v].get(x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = rstd * (dh[v][e] - c0 - (x[e] - mean) * rstd * c1);
-            store8<T, VEC>(static_cast<T*>(p.dx) + at, (v * TPR + t) * 8, p.width, active, x);
+            for (int i = 0; i < 4; ++i) n[v][i] = mul2(both(rstd), fma2(n[v][i], m1, add2(dh[v][i], m0)));
+            store8<T, VEC>(static_cast<T*>(p.dx) + at, (v * TPR + t) * 8, p.width, active, n[v]);
         }
     }
     launch_dependents();
@@ -302,21 +325,22 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), NV == 1 && sizeof(T) == 2 
     float* const mine = p.partial + static_cast<long long>(blockIdx.x) * 2 * p.width;
 #pragma unroll 1
     for (int which = 0; which < (p.want_db ? 2 : 1); ++which) {
-        if (G == 1) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int col = (v * TPR + t) * 8 + e;
-                    if (col < p.width) mine[which * p.width + col] = which ? db[v][e] : dw[v][e];
-                }
-            continue;
-        }
-        __syncthreads();
+        if (G > 1) __syncthreads();
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) gather[(threadIdx.x / TPR) * kColumns + (v * TPR + t) * 8 + e] = which ? db[v][e] : dw[v][e];
+            for (int i = 0; i < 4; ++i) {
+                const int col = (v * TPR + t) * 8 + 2 * i;
+                float a, b;
+                unpair2(which ? db[v][i] : dw[v][i], a, b);
+                if (G > 1) {
+                    gather[(threadIdx.x / TPR) * kColumns + col] = a, gather[(threadIdx.x / TPR) * kColumns + col + 1] = b;
+                } else {
+                    if (col < p.width) mine[which * p.width + col] = a;
+                    if (col + 1 < p.width) mine[which * p.width + col + 1] = b;
+                }
+            }
+        if (G == 1) continue;
         __syncthreads();
         for (int col = threadIdx.x; col < p.width; col += cta_threads<TPR>()) {
             float s = 0.f;
