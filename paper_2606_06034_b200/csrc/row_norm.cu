@@ -371,7 +371,9 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, in
     }
 }
 
-constexpr int kForwardThreads = 2048, kBackwardThreads = 1024;  // threads that a launch brings per SM, at most
+// Threads that a launch brings per SM, at most: as many as are resident there (80 registers backward, 48 forward), so that no CTA is left for a second
+// round. 1 M rows of 128: backward 0.26 ms, with 1024 threads 0.31; forward 0.147, with 1024 0.156, with 1536 0.176.
+constexpr int kForwardThreads = 1280, kBackwardThreads = 768;
 
 // threads of a row; CTAs of a launch
 int row_threads(int width) { return width <= 128 ? 16 : width <= 512 ? 32 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512; }
