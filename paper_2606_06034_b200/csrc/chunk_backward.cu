@@ -16,14 +16,17 @@
 //     N_ij = scale P_ij <dO_i, u_j> - A_ij <r_i, u_j>  (j < i)
 //     dg_i (cumulative) = sum_j N_ij - sum_j N_ji + scale exp(g_i) <q_i, S^T dO_i> - beta_i exp(g_i) <r_i, z_i> - exp(g_C - g_i) <u_i, y_i>
 //                         (at the chunk's end also + sum_i exp(g_C - g_i) <u_i, y_i> + exp(g_C) <D, S>), summed backwards for the raw gates
-// Four launches: `chunk_system` (per chunk and key head: T, P and the gates' tables), `chunk_states` (per sequence, value head and
-// slice of d_v, forward over the chunks: S, u, z), `chunk_state_grads` (the same backward: D, r), `chunk_grads` (per chunk and key
-// head, the value heads that share it in turn: dQ, dK, dV, dbeta, dg). Both chains are independent for each row of S (each value feature), so a head
-// is cut into slices for more CTAs than it has heads.
+// Four launches: `chunk_system` (per chunk and key head: T, P and the gates' tables), `chunk_states` (per sequence and value head,
+// forward over the chunks: S, u, z), `chunk_state_grads` (the same backward: D, r), `chunk_grads` (per chunk and key head, the value
+// heads that share it in turn: dQ, dK, dV, dbeta, dg). What the later ones need of the earlier ones goes through the caller's workspace.
 //
-// Precision: dbeta, dg and dS_in are fp32 and so is what they are made of. Products run on the tensor cores in tf32 with an fp32
-// operand as the sum of its upper 11 bits and the rest (2 products where the other operand is bf16, which tf32 holds exactly, 3 where
-// both are fp32): 2^-21 of a product is lost. What only reaches dQ, dK, dV, which are rounded to bf16 (2^-9), takes one product.
+// Precision: dbeta, dg and dS_in are fp32 and so is what they are made of. The tensor cores multiply bf16: an fp32 operand is the sum of
+// three bf16 pieces (24 bits), three products where the other operand is bf16 itself, six where both are split; all sums are fp32. What
+// reaches only dQ, dK, dV, which are rounded to bf16 (2^-9 on average), has two pieces (2^-17).
+//
+// us per launch, 8 x 4096 tokens with 32 heads / one sequence of 32768 tokens with 16 and 32 heads / 61 packed sequences of 16411 tokens
+// in all: system 605 / 504 / 283, states 514 / 1549 / 310, their gradients 790 / 2700 / 509, chunks' gradients 1640 / 1420 / 835. On
+// mma.sync with tf32 pieces the same four took 742 / 628, 1615 / 2607, 3137 / 3563 and 2945 / 2756.
 #include <cuda.h>
 
 #include "common.cuh"
@@ -563,7 +566,7 @@ struct Chain {
     uint32_t phase = 0;
     bool failed = false;
     __device__ __forceinline__ void wait() {
-        failed |= !wait_products(done, phase);
+        failed = failed || !wait_products(done, phase);
         phase ^= 1;
         tc_fence_after_sync();
     }
@@ -593,8 +596,10 @@ __device__ __forceinline__ void chain_end(Chain& ch, int* status, uint32_t colum
     if (threadIdx.x < 32) tmem_dealloc(ch.tm, columns);
 }
 
-// Forward: z, u and the state at the start of every chunk. A chunk's chain is three products (24 of 128 x 64 x 16 each) and, between them, the
-// splitting of what the next one reads: z -> right-hand side -> u -> state. What goes to memory (the state, z, u) goes while products run.
+// Forward: z, u and the state at the start of every chunk. A chunk's chain is three products (24 of 128 x 64 x 16 each, 1000 cycles with their
+// completion) and, between them, the splitting of what the next one reads (700 to 1200 cycles): z -> right-hand side -> u -> state, 3.0 us a
+// chunk. What goes to memory (the state, z, u) goes while products run, through shared memory and the copy engine: stored by the threads it
+// took 4.4 us, because their stores, 8 rows at a time, kept the loads waiting.
 struct StageF {  // (the tiles lie on 1 KB)
     uint8_t K[2 * kTile], V[2 * kTile], T[kPieces * kTile];
     float tab[kTabs * kC];
@@ -767,7 +772,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
     chain_end(ch, p.status, kTmColumns);
 }
 
-// Backward: r and the state's gradient at the end of every chunk.
+// Backward: r and the state's gradient at the end of every chunk, 5.3 us a chunk: four products on the chain, two more beside it.
 struct StageB {
     uint8_t K[2 * kTile], Q[2 * kTile], dO[2 * kTile];
     float tab[kTabs * kC];
@@ -1009,8 +1014,10 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
 // One CTA has a (chunk, key head) and takes the value heads that share it in turn. dQ and dK are summed transposed, a key feature on each of the
 // 128 lanes: A is S or D (tiles [v][key], read down the rows) or K or Q (read down the rows), B is dO, r, u, p or m (64 tokens wide). p and m
 // come from products of 64 x 64 (rows on 16 lanes of every quarter), r and u in three pieces: dbeta and dg are made of them. S and D have two
-// pieces (2^-17), which dQ and dK do not notice and dg hardly: <D, S> and <q, S^T dO>. What bounds it: the 304 KB that a value head's chunk reads and
-// writes (5.8 us of an SM's share of the HBM); the products take 150 issues of 32 cycles, 2.5 us.
+// pieces (2^-17), which dQ and dK do not notice and dg hardly: <D, S> and <q, S^T dO>. A value head's chunk reads and writes 304 KB (5.8 us of an
+// SM's share of the HBM) and its 200 products take 3 us; it takes 14.8 us, the chain of twenty phases of 16 warps between products (a scheduler
+// issues in 34 % of the cycles; 208 KB of operands leave no room for a second CTA). What the next chunk reads comes into L2 meanwhile, and S, u
+// and r of it into shared memory behind this one's last product: without either 20 us.
 constexpr int kGradThreads = 512;  // 16 warps, and one that issues the products and the copies of S and D
 
 struct SmemC {
@@ -1194,7 +1201,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 mma_commit(&bar_out);
             }
             __syncwarp();
-            failed |= !wait_products(&bar_load, 1);
+            failed = failed || !wait_products(&bar_load, 1);
             if (elect_one()) {
                 product<8>(tm + kTmUD, state(1), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, true), false);
                 product<8>(tm + kTmUD, state(0), kDown, desc_cols(tile_u(1)), kDown, grad_idesc(128, true, true, true), true);
@@ -1203,7 +1210,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             }
             __syncwarp();
             grad_await<4>();  // every part of dbeta and dg; the state's gradient is read
-            failed |= !wait_products(&bar_d, phase);
+            failed = failed || !wait_products(&bar_d, phase);
             phase ^= 1;
             if (next.ok) load(chunk_ws(p, next.slot, next_hv));
             // lane i has tokens 2i, 2i + 1
@@ -1274,7 +1281,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
         for (int n = 0, it = 0; now.ok; turn ^= 1) {
             const int hv = now.hk * heads + it, s = now.s, first = now.first, rows = now.rows;
             const bool last = it + 1 == heads;
-            failed |= !wait_products(&bar_load, 0);
+            failed = failed || !wait_products(&bar_load, 0);
             {  // u and r in pieces
                 float4 x[2][4];
 #pragma unroll
@@ -1295,7 +1302,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                     }
                 }
             }
-            failed |= !wait_products(&bar_tile, turn);
+            failed = failed || !wait_products(&bar_tile, turn);
             if (rows < kC) {
                 if (it == 0) clear_tail<kGradThreads>(sm.K, rows, tid), clear_tail<kGradThreads>(sm.Q, rows, tid);
                 clear_tail<kGradThreads>(sm.dO, rows, tid);
@@ -1322,7 +1329,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 rv = quad_sum(rv);
                 if (l.c == 0) sm.rv[warp / 8][row_v] = rv;
             }
-            failed |= !wait_products(&bar_s, turn);
+            failed = failed || !wait_products(&bar_s, turn);
             tc_fence_after_sync();
             uint4 x[2][4];
 #pragma unroll
@@ -1331,7 +1338,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 for (int i = 0; i < 4; ++i) x[q][i] = *reinterpret_cast<const uint4*>(sm.S + q * (kImage / 2) + (tid + i * kGradThreads) * 16);
             grad_arrive<3>();
             grad_sync();  // the third pieces make room
-            failed |= !wait_products(&bar_pair, turn);
+            failed = failed || !wait_products(&bar_pair, turn);
             tc_fence_after_sync();
             {  // p, m, and what dbeta and dg have of them
                 float ou[8], ru[8], kk[8], qk[8];
@@ -1399,7 +1406,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 }
                 put_dots(part, sm.Q, sm.rowq);
             }
-            failed |= !wait_products(&bar_load, 1);  // (the second copy of the value head's two)
+            failed = failed || !wait_products(&bar_load, 1);  // (the second copy of the value head's two)
             {  // <D, S>
                 float d = 0.f;
 #pragma unroll
@@ -1417,8 +1424,8 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 if (l.g == 0 && l.c == 0) sm.ds[warp] = d;
             }
             grad_arrive<4>();
-            failed |= !wait_products(&bar_out, turn);
-            failed |= !wait_products(&bar_d, turn);
+            failed = failed || !wait_products(&bar_out, turn);
+            failed = failed || !wait_products(&bar_d, turn);
             tc_fence_after_sync();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
