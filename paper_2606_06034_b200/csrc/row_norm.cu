@@ -283,7 +283,8 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), NV == 1 && sizeof(T) == 2 
         for (int v = 0; v < NV; ++v) raw[v] = next[v], gate[v] = next_gate[v], up[v] = next_up[v];
         if (first + step < p.rows) ask(row + step);
         f2 n[NV][4], dh[NV][4];
-        const float rstd = centred<T, NV, TPR, VEC>(raw, n, t, p, box, turn);
+        // (a row past the last is a row of zeros, whose rstd is infinite where eps = 0: 0, lest n be NaN)
+        const float inv = centred<T, NV, TPR, VEC>(raw, n, t, p, box, turn), rstd = active ? inv : 0.f;
         // dh, its sums, the gate's gradient. Elements past the width, and rows past the last, have dy = 0 and n = 0 and so count for nothing.
         f2 c0 = both(0.f), c1 = both(0.f);
 #pragma unroll
