@@ -430,9 +430,10 @@ int launch_layer_norm(const ProblemN& q, bool backward, cudaStream_t stream) {
     p.rows = q.rows, p.width = q.width, p.eps = q.eps, p.inv_width = 1.f / static_cast<float>(q.width);
     p.rms = (q.flags & GDN_NORM_RMS) != 0, p.param_bf16 = q.param_dtype == GDN_DTYPE_BF16;
     p.want_db = q.dbias != nullptr;
-    p.partial = backward && (q.dweight != nullptr || q.dbias != nullptr) ? static_cast<float*>(q.workspace) : nullptr;
+    const bool sums = backward && (q.dweight != nullptr || q.dbias != nullptr);
+    p.partial = sums ? static_cast<float*>(q.workspace) : nullptr;
     const int rc = q.dtype == GDN_DTYPE_BF16 ? launch_norm_width<__nv_bfloat16>(p, backward, stream) : launch_norm_width<float>(p, backward, stream);
-    if (rc != GDN_OK || p.partial == nullptr) return rc;
+    if (rc != GDN_OK || !sums) return rc;  // (without rows there is no workspace, and the sums are zero)
     const int parts = static_cast<int>(cta_count(q.rows, q.width, kBackwardThreads));
     float *const dw = q.dweight, *const db = q.dbias;
     const dim3 grid((q.width + 31) / 32, db != nullptr ? 2 : 1);  // (without a weight there may be a bias)

@@ -1,5 +1,7 @@
 """Row norms where a row group is not full, there is nothing to sum, or the gate's exponential leaves the middle of its range. Formula, inputs and
 tolerances as in test_gpu_norm.py unless a test says otherwise."""
+import ctypes
+
 import pytest
 import torch
 
@@ -15,3 +17,17 @@ pytestmark = pytest.mark.gpu
 def test_no_eps_and_rows_that_do_not_fill_a_group(dtype, rms, rows, width):
     """With eps = 0 a row of zeros has no norm: the places behind the last row hold such rows, and count for nothing in the weight's gradient."""
     _check(_inputs(rows, width, dtype, seed=rows), rms, eps=0.0)
+
+
+def test_no_rows_and_no_workspace():
+    """Nothing to sum: the library asks for no workspace, and the weight's and the bias's gradients are zero all the same."""
+    lib = gdn.load_library()
+    assert lib.gdn_layer_norm_backward_workspace(0, 128) == 0
+    some = torch.zeros(128, device="cuda")  # (rows of no tensor: an address that is neither read nor written)
+    dw, db = torch.full((128,), 7.0, device="cuda"), torch.full((128,), 7.0, device="cuda")
+    at = some.data_ptr()
+    rc = lib.gdn_layer_norm_backward(at, at, at, at, None, 0, 128, ctypes.c_float(1e-5), gdn.GDN_DTYPE_FP32, gdn.GDN_DTYPE_FP32, at, dw.data_ptr(), db.data_ptr(),
+                                     None, None, 0, 0, torch.cuda.current_stream().cuda_stream)
+    assert rc == gdn.GDN_OK
+    torch.cuda.synchronize()
+    assert not dw.any() and not db.any() and not some.any()
