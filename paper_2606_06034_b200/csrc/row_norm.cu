@@ -146,18 +146,23 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float2* box, int& turn) 
     }
 }
 
-// sigmoid in four instructions (a product, 2^x, a sum, a reciprocal, both of these within 2 ulp); exp(-z) = inf gives 0. The gate's arithmetic is
-// what the forward kernel issues most of: with __expf and __fdividef 147 us for 1 M rows of 128, so 139.
+// sigmoid. bf16 rows: four instructions (a product, 2^x, a sum, a reciprocal, the last ones within 2 ulp); exp(-z) = inf gives 0. The gate's
+// arithmetic is what the forward kernel issues most of: with __expf and __fdividef 147 us for 1 M rows of 128, so 139. The exponent is rounded before
+// 2^x is taken, 2^-18 where |z| is near 80, and log2(e) is: up to 3.8e-6 of the result, a thousandth of its rounding to bf16. fp32 rows: expf and a
+// division, which round the result alone.
+template <typename T>
 __device__ __forceinline__ float sigmoid(float z) {
+    if (sizeof(T) == 4) return 1.f / (1.f + expf(-z));
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return r;
 }
-__device__ __forceinline__ f2 sigmoid(f2 z) {
+template <typename T>
+__device__ __forceinline__ f2 sigmoid2(f2 z) {
     float a, b;
     unpair2(z, a, b);
-    return pair2(sigmoid(a), sigmoid(b));
+    return pair2(sigmoid<T>(a), sigmoid<T>(b));
 }
 
 constexpr int kNormThreads = 256;
@@ -246,7 +251,7 @@ __global__ void __launch_bounds__(cta_threads<TPR>()) norm_forward_kernel(const 
                 f2 z[4];
                 gate[v].get(z);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[v][i] = mul2(x[v][i], mul2(z[i], sigmoid(z[i])));
+                for (int i = 0; i < 4; ++i) x[v][i] = mul2(x[v][i], mul2(z[i], sigmoid2<T>(z[i])));
             }
             store8<T, VEC>(static_cast<T*>(p.y) + at, (v * TPR + t) * 8, p.width, active, x[v]);
         }
@@ -300,7 +305,7 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), NV == 1 && sizeof(T) == 2 
                 load_param<VEC>(p.bias, p.param_bf16, (v * TPR + t) * 8, p.width, 0.f, b);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f2 s = sigmoid(z[i]), zs = mul2(z[i], s);
+                    const f2 s = sigmoid2<T>(z[i]), zs = mul2(z[i], s);
                     // silu'(z) = s + z s (1 - s)
                     const f2 slope = fma2(zs, fma2(s, both(-1.f), both(1.f)), s), h = fma2(n[v][i], w[i], b[i]);
                     z[i] = mul2(mul2(dh[v][i], h), slope);

@@ -31,3 +31,23 @@ def test_no_rows_and_no_workspace():
     assert rc == gdn.GDN_OK
     torch.cuda.synchronize()
     assert not dw.any() and not db.any() and not some.any()
+
+@pytest.mark.parametrize("width", [128, 75, 2048])
+def test_gates_far_below_zero_keep_fp32_rows_exact(width):
+    """y and dgate of fp32 rows, value by value, where silu is small: z from -85 to -40. The rows hold 1 and -1 and their RMS is 1, so no sum is rounded. Off
+    by at most, in steps of 2^-24: rsqrt 4, exp(-z) 2 (its sum with 1 and the quotient 2), three products 3: 11, and 12 for second order. dgate: the slope
+    s + z s (1 - s) is z s less a fortieth at most, s is off by 4, the product and the sum by 2, both times 41 / 39; rsqrt 4, products 3: 14, doubled for
+    a margin that an exponent rounded before exp is taken does not fit into (|z| log2(e) = 123, off by 2^-18, is 44 steps by itself, and log2(e) in fp32 17)."""
+    gen = torch.Generator().manual_seed(width)
+    z = (-85 + 45 * torch.rand(64, width, generator=gen)).cuda()
+    x = torch.where(torch.rand(64, width, generator=gen) < 0.5, -1.0, 1.0).cuda()  # (rms: n = x, no sum is rounded)
+    w = torch.ones(width, device="cuda")
+    z64 = z.double()
+    s = torch.sigmoid(z64)
+    y = gdn.layer_norm(x, w, gate=z, rms=True, eps=0.0).double()
+    off = ((y - x * z64 * s) / (z64 * s)).abs().max().item()
+    assert off <= 12 * 2 ** -24, off
+    dz = gdn.layer_norm_backward(torch.ones_like(x), x, w, gate=z, rms=True, eps=0.0)[3]
+    slope = s * (1 + z64 * (1 - s))
+    off = ((dz.double() - x * slope) / slope).abs().max().item()
+    assert off <= 28 * 2 ** -24, off
