@@ -393,11 +393,12 @@ size_t gdn_layer_norm_backward_workspace(long long rows, int width);
 unsigned int gdn_int8_lut_checksum(void);
 
 /*
- * Waits for `stream`, then returns and clears the status word the kernels of
+ * Waits for `stream`, then returns and clears the status the kernels of
  * this library write on the current device: GDN_OK, or GDN_ERR_TIMEOUT when a
  * bounded wait inside a kernel gave up (its outputs are then undefined), or
- * GDN_ERR_INVALID_ARG when gdn_recurrent_step met a slot it cannot use.
- * This is the only call that synchronises.
+ * GDN_ERR_INVALID_ARG when gdn_recurrent_step met a slot it cannot use. Where
+ * both have happened the first call returns the timeout and the next one the
+ * other. This is the only call that synchronises.
  */
 int gdn_device_status(gdn_stream_t stream);
 

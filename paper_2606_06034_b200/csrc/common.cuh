@@ -160,7 +160,7 @@ inline bool launch_behind(void (*kern)(P...), dim3 grid, unsigned threads, size_
 }
 
 // Status word written by kernels (one per device, static device memory).
-int* device_status_word();  // device address for the current device (nullptr on failure)
+int* device_status_word();  // device address for the current device (nullptr on failure): the word for waits, behind it that for arguments
 void count_launch();
 
 // Kernel launchers. Each returns a gdn_status and launches on `stream`.

@@ -7,9 +7,9 @@
 
 namespace gdn {
 
-// One status word per device that loads this library; kernels write GDN_ERR_TIMEOUT here
-// when a bounded wait gives up.
-__device__ int g_status_word = 0;
+// Status words of each device that loads this library: kernels write GDN_ERR_TIMEOUT into the first when a bounded wait gives up, and
+// GDN_ERR_INVALID_ARG into the second when they meet an argument in device memory that they cannot use. One does not hide the other.
+__device__ int g_status_word[2] = {0, 0};
 
 namespace {
 std::atomic<long long> g_launches{0};
@@ -429,13 +429,14 @@ int gdn_device_status(gdn_stream_t stream) {
     }
     int* addr = device_status_word();
     if (addr == nullptr) return GDN_ERR_LAUNCH;
-    int value = 0;
-    if (cudaMemcpy(&value, addr, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return GDN_ERR_LAUNCH;
-    if (value != 0) {
+    int words[2] = {0, 0};
+    if (cudaMemcpy(words, addr, sizeof(words), cudaMemcpyDeviceToHost) != cudaSuccess) return GDN_ERR_LAUNCH;
+    const int first = words[0] != 0 ? 0 : 1;
+    if (words[first] != 0) {
         const int zero = 0;
-        if (cudaMemcpy(addr, &zero, sizeof(int), cudaMemcpyHostToDevice) != cudaSuccess) return GDN_ERR_LAUNCH;
+        if (cudaMemcpy(addr + first, &zero, sizeof(int), cudaMemcpyHostToDevice) != cudaSuccess) return GDN_ERR_LAUNCH;
     }
-    return value;
+    return words[first];
 }
 
 int gdn_default_order(int C) {

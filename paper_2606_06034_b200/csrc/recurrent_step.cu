@@ -30,7 +30,7 @@ struct ParamsStep {
     void* S;
     const int* slots;  // may be null: sequence b's state is S[b]
     void* O;
-    int* status;
+    int* status;  // for slots that cannot be used
     Strides q, v, gate;  // q: Q and K; v: V and O
     int H_v, group, T, d_k, d_v, n_slots, slices;
     float scale;
@@ -218,8 +218,9 @@ int launch_step_types(ParamsStep& p, long long seqs, cudaStream_t stream) {
 
 int launch_recurrent_step(const ProblemStep& q, cudaStream_t stream) {
     ParamsStep p{};
-    p.status = device_status_word();
-    if (p.status == nullptr) return GDN_ERR_LAUNCH;
+    int* const status = device_status_word();
+    if (status == nullptr) return GDN_ERR_LAUNCH;
+    p.status = status + 1;
     p.Q = q.Q, p.K = q.K, p.V = q.V, p.beta = q.beta, p.g = q.g, p.S = q.S, p.slots = q.slots, p.O = q.O;
     p.H_v = q.H_v, p.group = q.H_v / q.H_k, p.T = q.T, p.d_k = q.d_k, p.d_v = q.d_v, p.n_slots = q.n_slots;
     p.scale = q.scale, p.l2norm = (q.flags & GDN_FLAG_K_L2NORM) != 0;
