@@ -329,6 +329,7 @@ int gdn_chunk_state_output_segmented_noalloc(const void* Q, const void* K, const
  *   is a padded row of the batch: nothing of it is read, its output is zero. No slot may appear twice and none may reach n_slots:
  *   of two sequences with the same slot the first in the batch is computed; the other, like one whose slot is out of range, gets the
  *   output zero, changes no state, and gdn_device_status reports GDN_ERR_INVALID_ARG.
+ * O_out may be V; otherwise neither O_out nor S may overlap another argument (GDN_ERR_INVALID_ARG).
  * Any T >= 0 (a long prompt is faster through gdn_gated_delta_layer), d_k and d_v up to 256 in multiples of 8.
  */
 int gdn_recurrent_step(const void* Q, const void* K, const void* V, const float* beta, const float* g, int B, int H_k, int H_v, int T,

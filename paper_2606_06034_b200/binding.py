@@ -633,7 +633,7 @@ def gated_delta_step(Q, K, V, beta, g_raw, S, slots=None, scale=None, *, token_m
     S_out), updated in place. Q, K [B,T,H_k,d], V [B,T,H_v,d] (bf16 or fp32), beta, g_raw [B,T,H_v] (token_major) or the head-major
     forms; T = 1 for ordinary decoding, more where several tokens of a sequence are known at once. slots: int32 CUDA tensor [B],
     the state of each sequence (negative: a padded row, whose output is zero; no slot twice, see the header); None: sequence b has state b.
-    Returns O like V."""
+    out: a tensor like V to write to; V itself is allowed, other arguments are refused. Returns O like V."""
     where = "gated_delta_step"
     B, H_k, H_v, T, d_k, d_v = _layer_shapes(where, Q, K, V, beta, g_raw, token_major, False, *_TOKEN_TYPES)
     if S.dim() != 4:

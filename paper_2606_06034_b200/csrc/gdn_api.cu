@@ -2,6 +2,7 @@
 #include <atomic>
 #include <cstdint>
 #include <initializer_list>
+#include <utility>
 
 #include "common.cuh"
 
@@ -32,6 +33,12 @@ int* device_status_word() {
 }
 
 namespace {
+
+// whether two runs of bytes have one in common
+bool overlap(const void* a, long long na, const void* b, long long nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && (x < y ? y - x < static_cast<uintptr_t>(na) : x - y < static_cast<uintptr_t>(nb));
+}
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -317,6 +324,12 @@ int gdn_recurrent_step(const void* Q, const void* K, const void* V, const float*
     if (d_k % 8 != 0 || d_v % 8 != 0 || d_k > 256 || d_v > 256) return GDN_ERR_UNSUPPORTED;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(beta) || !aligned16(g) || !aligned16(S) || !aligned16(O_out) || !aligned16(slots))
         return GDN_ERR_ALIGN;
+    // the CTAs of a head store O and S while others still read; V's rows alone are read by the threads that store those of O
+    const long long rows = static_cast<long long>(B) * T, e = dtype == GDN_DTYPE_BF16 ? 2 : 4, out = rows * H_v * d_v * e, key = rows * H_k * d_k * e,
+                    state = static_cast<long long>(n_slots) * H_v * d_v * d_k * (state_dtype == GDN_DTYPE_BF16 ? 2 : 4);
+    for (const auto& [p, bytes] : {std::pair<const void*, long long>{Q, key}, {K, key}, {beta, rows * H_v * 4}, {g, rows * H_v * 4}, {slots, slots != nullptr ? B * 4LL : 0}})
+        if (overlap(O_out, out, p, bytes) || overlap(S, state, p, bytes)) return GDN_ERR_INVALID_ARG;
+    if ((V != O_out && overlap(O_out, out, V, out)) || overlap(S, state, V, out) || overlap(S, state, O_out, out)) return GDN_ERR_INVALID_ARG;
     const int rc = check_arch();
     if (rc != GDN_OK || B == 0 || T == 0) return rc;
     return launch_recurrent_step(ProblemStep{Q, K, V, beta, g, S, slots, O_out, B, H_k, H_v, T, d_k, d_v, n_slots, scale, dtype, state_dtype, flags},

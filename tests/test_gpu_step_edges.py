@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2606_06034_b200 import binding as gdn
-from test_gpu_step import _inputs
+from test_gpu_step import TOL, _expected, _inputs, _near
 
 pytestmark = pytest.mark.gpu
 
@@ -17,3 +17,19 @@ def test_an_unusable_slot_does_not_hide_a_wait_that_ran_out():
     assert gdn.gdn_device_status() == gdn.GDN_ERR_TIMEOUT
     assert gdn.gdn_device_status() == gdn.GDN_ERR_INVALID_ARG
     assert gdn.gdn_device_status() == gdn.GDN_OK
+
+def test_outputs_that_lie_on_inputs():
+    """Slices of a head store outputs while others still read Q and K: refused. V's rows are read by the threads that store O's: allowed."""
+    Q, K, V, beta, g, S = _inputs(3, 2, 2, 2, 128, 128, torch.bfloat16, 6)
+    for out in (Q, K):
+        with pytest.raises(gdn.GdnError):
+            gdn.gated_delta_step(Q, K, V, beta, g, S, out=out)
+    both = torch.cat([V.flatten(), V.flatten()])
+    with pytest.raises(gdn.GdnError):  # O a row behind V
+        gdn.gated_delta_step(Q, K, both[:V.numel()].view_as(V), beta, g, S, out=both[128:128 + V.numel()].view_as(V))
+    ref = _expected(Q, K, V, beta, g, S, [(b, b) for b in range(3)])
+    beside = gdn.gated_delta_step(Q, K, both[:V.numel()].view_as(V), beta, g, S.clone(), out=both[V.numel():].view_as(V))  # side by side
+    _near(beside, ref[0], TOL[torch.bfloat16])
+    assert gdn.gated_delta_step(Q, K, V, beta, g, S, out=V) is V
+    _near(V, ref[0], TOL[torch.bfloat16])
+    _near(S, ref[1], TOL[torch.float32])
