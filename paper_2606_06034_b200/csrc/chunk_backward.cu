@@ -47,7 +47,7 @@ constexpr int kPieces = 3;
 constexpr int kWsT = 0, kWsP = kWsT + kPieces * kC * kC / 2, kWsS = kWsP + kPieces * kC * kC / 2, kWsDS = kWsS + kD * kD, kWsU = kWsDS + kD * kD;
 constexpr int kWsZ = kWsU + kC * kD;     // exp(g) z, then r in its place
 constexpr int kWsTab = kWsZ + kC * kD;   // tables of 64 floats each
-enum { TAB_EGK = 0, TAB_BETA, TAB_ECK, TAB_BEGK, TAB_SEGQ, TAB_G, TAB_RK, TAB_RQ, kTabs };
+enum { TAB_EGK = 0, TAB_BETA, TAB_ECK, TAB_BEGK, TAB_SEGQ, TAB_G, TAB_GLO, TAB_RK, TAB_RQ, kTabs };  // (G, GLO: see Gates)
 constexpr int kWsDots = kWsTab + kTabs * kC;  // exp(g) <r, z>, exp(g_C - g) <u, y>
 constexpr int kDots = 2;
 constexpr int kWsChunk = kWsDots + kDots * kC;
@@ -181,6 +181,14 @@ __device__ __forceinline__ void store_pieces(float* tiles, int row, int col, con
 }
 
 // ---------------------------------------------------------------- T, P and the gates' tables
+// Gates: the sums of a chunk's log-gates reach 50 in ordinary texts and 8192 where gates close, and a sum in fp32 would be off by 2^-19 to 2^-11,
+// as would every decay exp(g_i - g_j) between neighbours be, relatively (r, and with it dbeta, by 1.4e-6 for ordinary gates; dbeta and dg
+// by 4e-5 to 4e-4 for 8 to 60 closed ones). They are summed in fp64 and kept as hi + lo.
+__device__ __forceinline__ float exp_between(float hi, float lo, float hi0, float lo0) { return expf((hi - hi0) + (lo - lo0)); }
+__device__ __forceinline__ float exp_of(float hi, float lo) {  // (lo <= 2^-18 where exp is not 0)
+    const float e = expf(hi);
+    return fmaf(e, lo, e);
+}
 struct SmemSystem {
     union {
         struct {
@@ -191,7 +199,7 @@ struct SmemSystem {
         };
     };
     float kk[kC * kLdV], qk[kC * kLdV];
-    float rk[kC], rq[kC], g[kC], beta[kC];
+    float rk[kC], rq[kC], g[kC], glo[kC], beta[kC];
 };
 
 __global__ void __launch_bounds__(kThreads, 3) chunk_system_kernel(const ParamsB p) {
@@ -256,17 +264,21 @@ __global__ void __launch_bounds__(kThreads, 3) chunk_system_kernel(const ParamsB
                 b[e] = t + e < rows ? p.beta[at] : 0.f;
                 if (x[e] < -128.f) x[e] = -128.f;
             }
-            float sum = x[0] + x[1];
+            double sum = static_cast<double>(x[0]) + x[1];
             for (int o = 1; o < 32; o *= 2) {
-                const float y = __shfl_up_sync(0xffffffffu, sum, o);
+                const double y = __shfl_up_sync(0xffffffffu, sum, o);
                 if (static_cast<int>(threadIdx.x) >= o) sum += y;
             }
-            sm.g[t] = sum - x[1], sm.g[t + 1] = sum;
+            for (int e = 0; e < 2; ++e) {
+                const double g = e ? sum : sum - x[1];
+                sm.g[t + e] = static_cast<float>(g);
+                sm.glo[t + e] = static_cast<float>(g - sm.g[t + e]);
+            }
             sm.beta[t] = b[0], sm.beta[t + 1] = b[1];
         }
         __syncthreads();
         if (tid < kC) {
-            const float g = sm.g[tid], eg = expf(g), ec = expf(sm.g[kC - 1] - g), beta = sm.beta[tid], rk = sm.rk[tid], rq = sm.rq[tid];
+            const float g = sm.g[tid], lo = sm.glo[tid], eg = exp_of(g, lo), ec = exp_between(sm.g[kC - 1], sm.glo[kC - 1], g, lo), beta = sm.beta[tid], rk = sm.rk[tid], rq = sm.rq[tid];
             float* const tab = ws + kWsTab;
             const bool real = tid < rows;
             tab[TAB_EGK * kC + tid] = real ? eg * rk : 0.f;
@@ -275,6 +287,7 @@ __global__ void __launch_bounds__(kThreads, 3) chunk_system_kernel(const ParamsB
             tab[TAB_BEGK * kC + tid] = real ? beta * eg * rk : 0.f;
             tab[TAB_SEGQ * kC + tid] = real ? p.scale * eg * rq : 0.f;
             tab[TAB_G * kC + tid] = g;
+            tab[TAB_GLO * kC + tid] = lo;
             tab[TAB_RK * kC + tid] = rk;
             tab[TAB_RQ * kC + tid] = rq;
         }
@@ -284,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 3) chunk_system_kernel(const ParamsB
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = col + e;
-                const float gam = j <= row ? expf(sm.g[row] - sm.g[j]) : 0.f;
+                const float gam = j <= row ? exp_between(sm.g[row], sm.glo[row], sm.g[j], sm.glo[j]) : 0.f;
                 a[e] = j < row ? sm.beta[row] * gam * sm.kk[row * kLdV + j] : 0.f;
                 q[e] = j <= row ? gam * sm.qk[row * kLdV + j] : 0.f;
             }
@@ -600,7 +613,7 @@ __device__ __forceinline__ void chain_end(Chain& ch, int* status, uint32_t colum
 // completion) and, between them, the splitting of what the next one reads (700 to 1200 cycles): z -> right-hand side -> u -> state, 3.0 us a
 // chunk. What goes to memory (the state, z, u) goes while products run, through shared memory and the copy engine: stored by the threads it
 // took 4.4 us, because their stores, 8 rows at a time, kept the loads waiting.
-struct StageF {  // (the tiles lie on 1 KB)
+struct alignas(1024) StageF {  // (the tiles lie on 1 KB)
     uint8_t K[2 * kTile], V[2 * kTile], T[kPieces * kTile];
     float tab[kTabs * kC];
 };
@@ -654,7 +667,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             if (c < n && me == 0) {
                 StageF& st = sm.stage[c % 2];
                 const float* const ws = chunk_ws(p, seq.slot + c, h);
-                mbar_arrive_expect_tx(ch.full, sizeof(StageF));
+                mbar_arrive_expect_tx(ch.full, sizeof(st.K) + sizeof(st.V) + sizeof(st.T) + sizeof(st.tab));
                 load_tile(st.K, maps.K, p, p.H_k, s, seq.first + c * kC, hk, ch.full);
                 load_tile(st.V, maps.V, p, p.H_v, s, seq.first + c * kC, h, ch.full);
                 bulk_load(st.T, ws + kWsT, sizeof(st.T), ch.full);
@@ -757,7 +770,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             put_vt(sm.image, u, row0, quarter);
             fence_proxy_async_smem();
             arrive<6, kLoaders>();
-            const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
+            const float decay = exp_of(st.tab[TAB_G * kC + kC - 1], st.tab[TAB_GLO * kC + kC - 1]);
             ch.wait();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
@@ -773,7 +786,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
 }
 
 // Backward: r and the state's gradient at the end of every chunk, 5.3 us a chunk: four products on the chain, two more beside it.
-struct StageB {
+struct alignas(1024) StageB {
     uint8_t K[2 * kTile], Q[2 * kTile], dO[2 * kTile];
     float tab[kTabs * kC];
 };
@@ -842,7 +855,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
         const auto load = [&](int c) {
             if (c >= 0 && me == 0) {
                 StageB& st = sm.stage[c % 2];
-                mbar_arrive_expect_tx(ch.full, sizeof(StageB) + sizeof(sm.T) + sizeof(sm.P));
+                mbar_arrive_expect_tx(ch.full, sizeof(st.K) + sizeof(st.Q) + sizeof(st.dO) + sizeof(st.tab) + sizeof(sm.T) + sizeof(sm.P));
                 load_tile(st.K, maps.K, p, p.H_k, s, seq.first + c * kC, hk, ch.full);
                 load_tile(st.Q, maps.Q, p, p.H_k, s, seq.first + c * kC, hk, ch.full);
                 load_tile(st.dO, maps.dO, p, p.H_v, s, seq.first + c * kC, h, ch.full);
@@ -983,7 +996,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
                 const float sum = token_sum(dots[d], l);
                 if ((l.g & 1) == 0) sm.dots[warp % 4][d][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
             }
-            const float decay = expf(st.tab[TAB_G * kC + kC - 1]);
+            const float decay = exp_of(st.tab[TAB_G * kC + kC - 1], st.tab[TAB_GLO * kC + kC - 1]);
             asm volatile("bar.sync 7, %0;" ::"n"(kWorkers) : "memory");
             if (threadIdx.x < kDots * kC) {
                 const float* const at = &sm.dots[0][0][threadIdx.x];
@@ -1231,7 +1244,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             float dsum = 0.f;
 #pragma unroll
             for (int x = 0; x < kGradThreads / 32; ++x) dsum += sm.ds[x];
-            if (lane == 31) d[1] += ends + expf(sm.tab[TAB_G * kC + kC - 1]) * dsum;
+            if (lane == 31) d[1] += ends + exp_of(sm.tab[TAB_G * kC + kC - 1], sm.tab[TAB_GLO * kC + kC - 1]) * dsum;
             float sum = d[0] + d[1];
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
@@ -1347,7 +1360,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 tm_ld16(lanes + kTmKK, kk);
                 tm_ld16(lanes + kTmQK, qk);
                 tmem_wait_ld();
-                const float* const g = sm.tab + TAB_G * kC;
+                const float *const g = sm.tab + TAB_G * kC, *const lo = sm.tab + TAB_GLO * kC;
                 const float* const rk = sm.tab + TAB_RK * kC;
                 float rown[2] = {}, rowb[2] = {}, coln[4] = {};
 #pragma unroll
@@ -1357,7 +1370,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int j = j0 + e;
-                        const float gam = j <= i ? expf(g[i] - g[j]) * rk[j] : 0.f;
+                        const float gam = j <= i ? exp_between(g[i], lo[i], g[j], lo[j]) * rk[j] : 0.f;
                         // p_ij and m_ij with the lengths of the rows that they will multiply
                         pp[e] = j <= i ? ou[x + e] * (p.scale * gam * sm.tab[TAB_RQ * kC + i]) : 0.f;
                         const float kg = j < i ? -gam * rk[i] * ru[x + e] : 0.f;
