@@ -349,8 +349,9 @@ int gdn_recurrent_step(const void* Q, const void* K, const void* V, const float*
  *   workspace: DEVICE memory of gdn_gated_delta_layer_backward_workspace(B, B * T, H_v) bytes (B = 0 or T = 0: none), 16-byte
  *   aligned, owned by the caller and free to reuse when the stream has passed the call. It holds every chunk's state and its gradient; nothing
  *   is kept from the forward pass. Calls that may overlap need a workspace each.
- * The result does not depend on timing (no atomics). A log-gate below -128 counts as -128. dbeta, dg and dS_in are accurate to fp32
- * arithmetic; dQ, dK, dV to their rounding to bf16.
+ * The result does not depend on timing (no atomics). A log-gate below -128 counts as -128. All arithmetic is as accurate as fp32 (operands of the
+ * tensor cores keep 24 bits, a chunk's log-gates are summed in fp64); dQ, dK, dV are rounded to bf16 at the end.
+ * dS_in may be dS_out; apart from that no output and no workspace may overlap another argument.
  * Supported: C = 64, d_k = d_v = 128.
  */
 int gdn_gated_delta_layer_backward(const void* dO, const void* Q, const void* K, const void* V, const float* beta, const float* g, int B,

@@ -20,13 +20,15 @@
 // forward over the chunks: S, u, z), `chunk_state_grads` (the same backward: D, r), `chunk_grads` (per chunk and key head, the value
 // heads that share it in turn: dQ, dK, dV, dbeta, dg). What the later ones need of the earlier ones goes through the caller's workspace.
 //
-// Precision: dbeta, dg and dS_in are fp32 and so is what they are made of. The tensor cores multiply bf16: an fp32 operand is the sum of
-// three bf16 pieces (24 bits), three products where the other operand is bf16 itself, six where both are split; all sums are fp32. What
-// reaches only dQ, dK, dV, which are rounded to bf16 (2^-9 on average), has two pieces (2^-17).
+// Precision: everything between the bf16 inputs and the results is fp32. The tensor cores multiply bf16: an fp32 operand is the sum of three
+// bf16 pieces (24 bits), three products where the other operand is bf16 itself, six where both are split (the three smallest of the nine are
+// below 2^-24); all sums are fp32. The one rounding to fewer bits is that of dQ, dK, dV to bf16 at their end. Against fp64, relative 2-norms: dbeta
+// 1.8e-7 to 2.8e-7, dg 1.6e-7 to 7e-7, dS_in 5e-8 to 2.2e-7 (the formulas in torch fp32: 2.1e-7 to 7e-7, 1.2e-7 to 1.8e-6, 6e-8 to 1.5e-7).
 //
 // us per launch, 8 x 4096 tokens with 32 heads / one sequence of 32768 tokens with 16 and 32 heads / 61 packed sequences of 16411 tokens
-// in all: system 605 / 504 / 283, states 514 / 1549 / 310, their gradients 790 / 2700 / 509, chunks' gradients 1640 / 1420 / 835. On
-// mma.sync with tf32 pieces the same four took 742 / 628, 1615 / 2607, 3137 / 3563 and 2945 / 2756.
+// in all: system 621 / 521 / 297, states 498 / 1512 / 306, their gradients 747 / 2658 / 488, chunks' gradients 1740 / 1526 / 948. (With
+// states, p and m of two pieces in the last one, 1507 / 1450 / 852: dg was off by 3.4e-6 where <D, S> is all of it, and three times as many values of
+// dQ, dK fell on the other side of a rounding.) On mma.sync with tf32 pieces the four took 742 / 628, 1615 / 2607, 3137 / 3563 and 2945 / 2756.
 #include <cuda.h>
 
 #include "common.cuh"
@@ -40,14 +42,14 @@ using namespace sm100;
 constexpr int kC = 64, kD = 128;
 constexpr int kThreads = 256;
 
-// workspace of one chunk of one value head, in floats. T and P: bf16 tiles of three pieces each (see split3); the states: tiles [v][64 keys] of
-// the upper two pieces; all as the products want them in shared memory. u, z, r [v][token] fp32: a feature of the value per row, as the
+// workspace of one chunk of one value head, in floats. T and P: bf16 tiles of three pieces each (see split3), as the products want them in shared
+// memory. The states [v][key] fp32, in blocks of 8 x 8 (see state_at). u, z, r [v][token] fp32: a feature of the value per row, as the
 // chains have them in tensor memory, 16-byte pieces of a row out of order (see vt_at).
 constexpr int kPieces = 3;
 constexpr int kWsT = 0, kWsP = kWsT + kPieces * kC * kC / 2, kWsS = kWsP + kPieces * kC * kC / 2, kWsDS = kWsS + kD * kD, kWsU = kWsDS + kD * kD;
 constexpr int kWsZ = kWsU + kC * kD;     // exp(g) z, then r in its place
 constexpr int kWsTab = kWsZ + kC * kD;   // tables of 64 floats each
-enum { TAB_EGK = 0, TAB_BETA, TAB_ECK, TAB_BEGK, TAB_SEGQ, TAB_G, TAB_GLO, TAB_RK, TAB_RQ, kTabs };  // (G, GLO: see Gates)
+enum { TAB_EGK = 0, TAB_BETA, TAB_ECK, TAB_BEGK, TAB_SEGQ, TAB_G, TAB_GLO, TAB_RK, TAB_RQ, TAB_DECAY, kTabs };  // (G, GLO: see Gates; DECAY: exp(g_C), at 0)
 constexpr int kWsDots = kWsTab + kTabs * kC;  // exp(g) <r, z>, exp(g_C - g) <u, y>
 constexpr int kDots = 2;
 constexpr int kWsChunk = kWsDots + kDots * kC;
@@ -288,6 +290,7 @@ __global__ void __launch_bounds__(kThreads, 3) chunk_system_kernel(const ParamsB
             tab[TAB_SEGQ * kC + tid] = real ? p.scale * eg * rq : 0.f;
             tab[TAB_G * kC + tid] = g;
             tab[TAB_GLO * kC + tid] = lo;
+            if (tid == kC - 1) tab[TAB_DECAY * kC] = eg;
             tab[TAB_RK * kC + tid] = rk;
             tab[TAB_RQ * kC + tid] = rq;
         }
@@ -530,9 +533,9 @@ __device__ __forceinline__ void for_pairs(const F& f) {
 
 constexpr int kLoaders = 32;
 constexpr int kChainThreads = kWorkers + 32 + kLoaders;  // sixteen warps that compute, one that issues the products, one that asks for tiles and has them stored
-constexpr int kImage = 2 * 2 * 2 * kTile;     // bytes of a state's tiles: two pieces of two tiles of 128 rows
-// Byte of element (row, col) of a state in its image
-__device__ __forceinline__ int image_at(int piece, int row, int col) { return (piece * 2 + col / 64) * 2 * kTile + swizzled(row, col % 64); }
+constexpr int kImage = kD * kD * 4;  // bytes of a state
+// Byte of element (row, col) of a state: blocks of 8 x 8 values, which a warp writes at once
+__device__ __forceinline__ int state_at(int row, int col) { return (row / 8 * (kD / 8) + col / 8) * 256 + row % 8 * 32 + col % 8 * 4; }
 // Byte of element (row, token) of u, z or r: 16-byte pieces change places, two by two, with the row's number mod 8: what a warp writes at once (8
 // rows of 8 tokens) lies on all banks
 __device__ __forceinline__ int vt_at(int row, int t) { return row * (kC * 4) + ((((t >> 2) ^ (row << 1)) & 15) << 4) + (t & 3) * 4; }
@@ -549,11 +552,7 @@ __device__ __forceinline__ void put_image(uint8_t* image, const float (&S)[2][16
 #pragma unroll
     for (int lh = 0; lh < 2; ++lh)
         for_pairs<16>([&](int row, int col, int i) {
-            const uint32_t h = pack_bf16x2(S[lh][i], S[lh][i + 1]);
-            const uint32_t m = pack_bf16x2(bf16_minus_lo(h, S[lh][i]), bf16_minus_hi(h, S[lh][i + 1]));
-            uint8_t* const at = image + image_at(0, row0 + lh * 16 + row, quarter * 32 + col);
-            *reinterpret_cast<uint32_t*>(at) = h;
-            *reinterpret_cast<uint32_t*>(at + kImage / 2) = m;
+            *reinterpret_cast<float2*>(image + state_at(row0 + lh * 16 + row, quarter * 32 + col)) = make_float2(S[lh][i], S[lh][i + 1]);
         });
 }
 
@@ -770,7 +769,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_states_kernel(const Pa
             put_vt(sm.image, u, row0, quarter);
             fence_proxy_async_smem();
             arrive<6, kLoaders>();
-            const float decay = exp_of(st.tab[TAB_G * kC + kC - 1], st.tab[TAB_GLO * kC + kC - 1]);
+            const float decay = st.tab[TAB_DECAY * kC];
             ch.wait();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
@@ -996,7 +995,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
                 const float sum = token_sum(dots[d], l);
                 if ((l.g & 1) == 0) sm.dots[warp % 4][d][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
             }
-            const float decay = exp_of(st.tab[TAB_G * kC + kC - 1], st.tab[TAB_GLO * kC + kC - 1]);
+            const float decay = st.tab[TAB_DECAY * kC];
             asm volatile("bar.sync 7, %0;" ::"n"(kWorkers) : "memory");
             if (threadIdx.x < kDots * kC) {
                 const float* const at = &sm.dots[0][0][threadIdx.x];
@@ -1026,18 +1025,18 @@ __global__ void __launch_bounds__(kChainThreads, 1) chunk_state_grads_kernel(con
 // ---------------------------------------------------------------- the chunks' gradients
 // One CTA has a (chunk, key head) and takes the value heads that share it in turn. dQ and dK are summed transposed, a key feature on each of the
 // 128 lanes: A is S or D (tiles [v][key], read down the rows) or K or Q (read down the rows), B is dO, r, u, p or m (64 tokens wide). p and m
-// come from products of 64 x 64 (rows on 16 lanes of every quarter), r and u in three pieces: dbeta and dg are made of them. S and D have two
-// pieces (2^-17), which dQ and dK do not notice and dg hardly: <D, S> and <q, S^T dO>. A value head's chunk reads and writes 304 KB (5.8 us of an
-// SM's share of the HBM) and its 200 products take 3 us; it takes 14.8 us, the chain of twenty phases of 16 warps between products (a scheduler
-// issues in 34 % of the cycles; 208 KB of operands leave no room for a second CTA). What the next chunk reads comes into L2 meanwhile, and S, u
-// and r of it into shared memory behind this one's last product: without either 20 us.
+// come from products of 64 x 64 (rows on 16 lanes of every quarter). Everything fp32 has three pieces. Those of S or D take 96 KB, and 64 are free: the
+// third one takes the place of the second when this one's products are done (S), or that of p and m (D). A value head's chunk reads and writes 307 KB
+// (6.9 us of an SM's share of the measured HBM rate); it takes 15.7 us, the chain of some twenty phases of 16 warps between 256 products. 208 KB of
+// operands leave no room for a second CTA. The products of pairs, which do not need S, run while S is split: 1.87 -> 1.74 ms for 16384 chunks. What
+// the next chunk reads comes into L2 meanwhile, and S, u and r of it into shared memory behind this one's last product: without either 20 us.
 constexpr int kGradThreads = 512;  // 16 warps, and one that issues the products and the copies of S and D
 
 struct SmemC {
     uint8_t K[2 * kTile], Q[2 * kTile], dO[2 * kTile];
-    uint8_t S[kImage];                                     // the state, then its gradient
-    // [v][token] in pieces. Before that u and r as they come, in the first 64 KB; later p and m in the place of the third pieces, two
-    // pieces each; at the end dQ and dK on their way out, in the last 32 KB
+    uint8_t S[kImage];                                     // the state, then its gradient, as they come; then two pieces, tiles [v][64 keys]
+    // [v][token] in pieces. Before that u and r as they come, in the first 64 KB; later p and m in the place of r, three pieces each, and
+    // the third piece of the state's gradient in the place of p and m; at the end dQ and dK on their way out, in the last 32 KB
     uint8_t u[kPieces][2 * kTile], r[kPieces][2 * kTile];
     float tab[kTabs * kC];
     float rowq[4][kC], rown[4][kC], rowb[4][kC], coln[4][kC], rv[2][kC], norm[2][4][kC];
@@ -1076,7 +1075,7 @@ constexpr uint32_t kTmDOS = 0, kTmRS = 64, kTmUD = 128, kTmDQ = 192, kTmDK = 256
 __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const ParamsB p, const __grid_constant__ Maps maps) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SmemC& sm = *reinterpret_cast<SmemC*>(smem_raw + ((0u - smem_u32(smem_raw)) & 1023u));
-    __shared__ uint64_t bar_pair, bar_s, bar_out, bar_d, bar_load, bar_tile;
+    __shared__ uint64_t bar_pair, bar_s, bar_l, bar_out, bar_d, bar_load, bar_tile;
     __shared__ uint32_t base;
     __shared__ Unit units[2];
     const int tid = threadIdx.x, warp = tid / 32;
@@ -1096,7 +1095,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
     };
     if (tid == 0) {
         units[0] = find_unit(blockIdx.x);
-        for (uint64_t* b : {&bar_pair, &bar_s, &bar_out, &bar_d, &bar_load, &bar_tile}) mbar_init(b, 1);
+        for (uint64_t* b : {&bar_pair, &bar_s, &bar_l, &bar_out, &bar_d, &bar_load, &bar_tile}) mbar_init(b, 1);
         mbar_fence_init();
     }
     if (warp == 0) {
@@ -1114,6 +1113,16 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
         const auto tile_u = [&](int i) { return smem_u32(sm.u[i]); };
         const auto tile_r = [&](int i) { return smem_u32(sm.r[i]); };
         const auto state = [&](int i) { return smem_desc(S + i * (kImage / 2), 2 * kTile, 1024, SWZ_128B); };
+        // a state's second piece times the upper two of u or r, and its first one times all three. (The third one's product comes on its own.)
+        const auto products_second = [&](uint32_t d, const auto& tile) {
+            product<8>(d, state(1), kDown, desc_cols(tile(1)), kDown, grad_idesc(128, true, true, false), false);
+            product<8>(d, state(1), kDown, desc_cols(tile(0)), kDown, grad_idesc(128, true, true, true), true);
+        };
+        const auto products_first = [&](uint32_t d, const auto& tile) {
+            product<8>(d, state(0), kDown, desc_cols(tile(2)), kDown, grad_idesc(128, true, true, false), true);
+            product<8>(d, state(0), kDown, desc_cols(tile(1)), kDown, grad_idesc(128, true, true, true), true);
+            product<8>(d, state(0), kDown, desc_cols(tile(0)), kDown, grad_idesc(128, true, true, false), true);
+        };
         // What is asked for next comes into L2 while the products of the present head run: the HBM would idle then, and be what everybody
         // waits for later
         const auto prefetch = [&](const Unit& x, int hv, bool keys) {
@@ -1166,17 +1175,8 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 __syncwarp();
             }
             const int next_hv = last ? next.hk * heads : hv + 1;
-            grad_await<1>();  // K, Q, dO, u, r are there
+            grad_await<7>();  // K, Q, dO, u, r are there
             tc_fence_after_sync();
-            if (elect_one()) {
-                product<8>(tm + kTmDOS, state(1), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, true), false);
-                product<8>(tm + kTmDOS, state(0), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, false), true);
-                product<8>(tm + kTmRS, state(1), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, true), false);
-                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(1)), kDown, grad_idesc(128, true, true, true), true);
-                product<8>(tm + kTmRS, state(0), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, false), true);
-                mma_commit(&bar_s);
-            }
-            __syncwarp();
             if (elect_one()) {
 #pragma unroll
                 for (int i = kPieces - 1; i >= 0; --i)
@@ -1192,9 +1192,27 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 mma_commit(&bar_pair);
             }
             __syncwarp();
-            prefetch(next, next_hv, last);
-            grad_await<3>();  // the state is used up
+            grad_await<1>();  // the state
+            tc_fence_after_sync();
             if (elect_one()) {
+                product<8>(tm + kTmDOS, state(1), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, true), false);
+                products_second(tm + kTmRS, tile_r);
+                mma_commit(&bar_s);  // the second piece is used up: the third one may have its place
+                product<8>(tm + kTmDOS, state(0), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, false), true);
+                products_first(tm + kTmRS, tile_r);
+            }
+            __syncwarp();
+            prefetch(next, next_hv, last);
+            grad_await<3>();  // the state's third piece
+            tc_fence_after_sync();
+            if (elect_one()) {
+                product<8>(tm + kTmDOS, state(1), kDown, desc_rows(dO), kAlong, grad_idesc(128, true, false, false), true);
+                product<8>(tm + kTmRS, state(1), kDown, desc_cols(tile_r(0)), kDown, grad_idesc(128, true, true, false), true);
+                mma_commit(&bar_l);
+            }
+            __syncwarp();
+            failed = failed || !wait_products(&bar_l, phase);
+            if (elect_one()) {  // the state is used up
                 mbar_arrive_expect_tx(&bar_load, kImage);
                 bulk_load(sm.S, ws + kWsDS, kImage, &bar_load);
             }
@@ -1204,25 +1222,27 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             if (elect_one()) {
                 const uint64_t Kd = desc_cols(K), Qd = desc_cols(Q);
 #pragma unroll
-                for (int i = 1; i >= 0; --i) {
-                    const uint32_t pt = tile_u(2) + i * kTile, mt = tile_r(2) + i * kTile;
-                    product<4>(tm + kTmDQ, Kd, kDown, desc_rows(pt), kAlong, grad_idesc(128, true, false, i == 1), i == 0);
-                    product<4>(tm + kTmDK, Qd, kDown, desc_cols(pt), kDown, grad_idesc(128, true, true, i == 1), i == 0);
+                for (int i = kPieces - 1; i >= 0; --i) {
+                    const uint32_t pt = tile_r(0) + i * kTile, mt = pt + kPieces * kTile;
+                    product<4>(tm + kTmDQ, Kd, kDown, desc_rows(pt), kAlong, grad_idesc(128, true, false, i == 1), i < kPieces - 1);
+                    product<4>(tm + kTmDK, Qd, kDown, desc_cols(pt), kDown, grad_idesc(128, true, true, i == 1), i < kPieces - 1);
                     product<4>(tm + kTmDK, Kd, kDown, desc_rows(mt), kAlong, grad_idesc(128, true, false, i == 1), true);
                     product<4>(tm + kTmDK, Kd, kDown, desc_cols(mt), kDown, grad_idesc(128, true, true, i == 1), true);
                 }
                 mma_commit(&bar_out);
             }
             __syncwarp();
-            failed = failed || !wait_products(&bar_load, 1);
+            grad_await<6>();  // the state's gradient
+            tc_fence_after_sync();
+            if (elect_one()) products_second(tm + kTmUD, tile_u), products_first(tm + kTmUD, tile_u);
+            __syncwarp();
+            grad_await<4>();  // its third piece, where p and m were; every part of dbeta and dg
+            tc_fence_after_sync();
             if (elect_one()) {
-                product<8>(tm + kTmUD, state(1), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, true), false);
-                product<8>(tm + kTmUD, state(0), kDown, desc_cols(tile_u(1)), kDown, grad_idesc(128, true, true, true), true);
-                product<8>(tm + kTmUD, state(0), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, false), true);
+                product<8>(tm + kTmUD, smem_desc(tile_r(0), 2 * kTile, 1024, SWZ_128B), kDown, desc_cols(tile_u(0)), kDown, grad_idesc(128, true, true, false), true);
                 mma_commit(&bar_d);
             }
             __syncwarp();
-            grad_await<4>();  // every part of dbeta and dg; the state's gradient is read
             failed = failed || !wait_products(&bar_d, phase);
             phase ^= 1;
             if (next.ok) load(chunk_ws(p, next.slot, next_hv));
@@ -1244,7 +1264,7 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             float dsum = 0.f;
 #pragma unroll
             for (int x = 0; x < kGradThreads / 32; ++x) dsum += sm.ds[x];
-            if (lane == 31) d[1] += ends + exp_of(sm.tab[TAB_G * kC + kC - 1], sm.tab[TAB_GLO * kC + kC - 1]) * dsum;
+            if (lane == 31) d[1] += ends + sm.tab[TAB_DECAY * kC] * dsum;
             float sum = d[0] + d[1];
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
@@ -1278,6 +1298,30 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             }
             const float sum = token_sum(d, l);
             if ((l.g & 1) == 0) to[quad][quarter * 16 + (l.g >> 2) * 8 + 2 * l.c + ((l.g >> 1) & 1)] = sum;
+        };
+        // This thread's part of a state, 8 x 4 values: as it has come, and the places of its pieces. The pieces take the place of the fp32 values, so every
+        // thread reads before any of them writes; the third one comes where the second is when that has been used.
+        const auto state_of = [&](int i) { return reinterpret_cast<const float4*>(sm.S) + tid + i * kGradThreads; };
+        const auto place_of = [&](int i) {
+            const int at = tid + i * kGradThreads, row = at / 256 * 8 + at % 16 / 2, col = at / 16 % 16 * 8 + at % 2 * 4;
+            return col / 64 * 2 * kTile + swizzled(row, col % 64);
+        };
+        const auto put_two = [&](const float4 (&x)[8], uint2 (&third)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint2 h, m;
+                split3(x[i].x, x[i].y, h.x, m.x, third[i].x);
+                split3(x[i].z, x[i].w, h.y, m.y, third[i].y);
+                const int place = place_of(i);
+                *reinterpret_cast<uint2*>(sm.S + place) = h;
+                *reinterpret_cast<uint2*>(sm.S + kImage / 2 + place) = m;
+            }
+            fence_proxy_async_smem();
+        };
+        const auto put_third = [&](uint8_t* to, const uint2 (&third)[8]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2*>(to + place_of(i)) = third[i];
+            fence_proxy_async_smem();
         };
         // V for <r, v>, eight tokens a warp and half of the features
         uint32_t v[8];
@@ -1321,8 +1365,16 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 clear_tail<kGradThreads>(sm.dO, rows, tid);
             }
             fence_proxy_async_smem();
-            grad_arrive<1>();
-            grad_sync();
+            grad_arrive<7>();
+            uint2 third[8];
+            {  // the state in pieces
+                float4 x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = *state_of(i);
+                grad_sync();
+                put_two(x, third);
+                grad_arrive<1>();
+            }
             {  // dV = beta r, turned back, and <r, v>
                 const float b = sm.tab[TAB_BETA * kC + row_v];
                 const long long at_v = p.v.at(s, first + row_v, hv) + warp / 8 * 64 + 2 * l.c;
@@ -1344,13 +1396,8 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
             }
             failed = failed || !wait_products(&bar_s, turn);
             tc_fence_after_sync();
-            uint4 x[2][4];
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[q][i] = *reinterpret_cast<const uint4*>(sm.S + q * (kImage / 2) + (tid + i * kGradThreads) * 16);
+            put_third(sm.S + kImage / 2, third);
             grad_arrive<3>();
-            grad_sync();  // the third pieces make room
             failed = failed || !wait_products(&bar_pair, turn);
             tc_fence_after_sync();
             {  // p, m, and what dbeta and dg have of them
@@ -1363,32 +1410,34 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 const float *const g = sm.tab + TAB_G * kC, *const lo = sm.tab + TAB_GLO * kC;
                 const float* const rk = sm.tab + TAB_RK * kC;
                 float rown[2] = {}, rowb[2] = {}, coln[4] = {};
+                float pp[8], mm[8];  // p_ij and m_ij with the lengths of the rows that they will multiply
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const int i = quad * 16 + ((x >> 1) & 1) * 8 + l.g, j = t0 + (x >> 2) * 8 + (x & 1);
+                    const float gam = j <= i ? exp_between(g[i], lo[i], g[j], lo[j]) * rk[j] : 0.f;
+                    pp[x] = j <= i ? ou[x] * (p.scale * gam * sm.tab[TAB_RQ * kC + i]) : 0.f;
+                    const float kg = j < i ? -gam * rk[i] * ru[x] : 0.f;
+                    mm[x] = sm.tab[TAB_BETA * kC + i] * kg;
+                    if (j < i) {
+                        const float both = fmaf(pp[x], qk[x], mm[x] * kk[x]);
+                        rown[(x >> 1) & 1] += both;
+                        coln[(x >> 2) * 2 + (x & 1)] += both;
+                        rowb[(x >> 1) & 1] = fmaf(kg, kk[x], rowb[(x >> 1) & 1]);
+                    }
+                }
+                // they take the place of r: every thread had read it when the products that bar_l stands for were asked for, and these were its last
+                failed = failed || !wait_products(&bar_l, turn);
+                tc_fence_after_sync();
 #pragma unroll
                 for (int x = 0; x < 8; x += 2) {
-                    const int i = quad * 16 + ((x >> 1) & 1) * 8 + l.g, j0 = t0 + (x >> 2) * 8;
-                    float pp[2], mm[2];
+                    uint32_t w[kPieces];
+                    uint8_t* const at = sm.r[0] + swizzled(quad * 16 + ((x >> 1) & 1) * 8 + l.g, t0 + (x >> 2) * 8);
+                    split3(pp[x], pp[x + 1], w[0], w[1], w[2]);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int j = j0 + e;
-                        const float gam = j <= i ? exp_between(g[i], lo[i], g[j], lo[j]) * rk[j] : 0.f;
-                        // p_ij and m_ij with the lengths of the rows that they will multiply
-                        pp[e] = j <= i ? ou[x + e] * (p.scale * gam * sm.tab[TAB_RQ * kC + i]) : 0.f;
-                        const float kg = j < i ? -gam * rk[i] * ru[x + e] : 0.f;
-                        mm[e] = sm.tab[TAB_BETA * kC + i] * kg;
-                        if (j < i) {
-                            const float both = fmaf(pp[e], qk[x + e], mm[e] * kk[x + e]);
-                            rown[(x >> 1) & 1] += both;
-                            coln[(x >> 2) * 2 + e] += both;
-                            rowb[(x >> 1) & 1] = fmaf(kg, kk[x + e], rowb[(x >> 1) & 1]);
-                        }
-                    }
-                    const int place = swizzled(i, j0);
-                    uint32_t h = pack_bf16x2(pp[0], pp[1]);
-                    *reinterpret_cast<uint32_t*>(sm.u[2] + place) = h;
-                    *reinterpret_cast<uint32_t*>(sm.u[2] + kTile + place) = pack_bf16x2(bf16_minus_lo(h, pp[0]), bf16_minus_hi(h, pp[1]));
-                    h = pack_bf16x2(mm[0], mm[1]);
-                    *reinterpret_cast<uint32_t*>(sm.r[2] + place) = h;
-                    *reinterpret_cast<uint32_t*>(sm.r[2] + kTile + place) = pack_bf16x2(bf16_minus_lo(h, mm[0]), bf16_minus_hi(h, mm[1]));
+                    for (int q = 0; q < kPieces; ++q) *reinterpret_cast<uint32_t*>(at + q * kTile) = w[q];
+                    split3(mm[x], mm[x + 1], w[0], w[1], w[2]);
+#pragma unroll
+                    for (int q = 0; q < kPieces; ++q) *reinterpret_cast<uint32_t*>(at + (kPieces + q) * kTile) = w[q];
                 }
                 fence_proxy_async_smem();
                 tc_fence_before_sync();
@@ -1419,39 +1468,47 @@ __global__ void __launch_bounds__(kGradThreads + 32, 1) chunk_grads_kernel(const
                 }
                 put_dots(part, sm.Q, sm.rowq);
             }
-            failed = failed || !wait_products(&bar_load, 1);  // (the second copy of the value head's two)
-            {  // <D, S>
+            {  // <D, S>, both in fp32: S comes again, from L2
+                const float4* const again = reinterpret_cast<const float4*>(chunk_ws(p, now.slot, hv) + kWsS) + tid;
+                float4 x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = again[i * kGradThreads];
+                failed = failed || !wait_products(&bar_load, 1);  // (the second copy of the value head's two)
                 float d = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint4 h4 = *reinterpret_cast<const uint4*>(sm.S + (tid + i * kGradThreads) * 16), m4 = *reinterpret_cast<const uint4*>(sm.S + kImage / 2 + (tid + i * kGradThreads) * 16);
-                    const uint32_t a[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w}, b[4] = {x[1][i].x, x[1][i].y, x[1][i].z, x[1][i].w};
-                    const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, m[4] = {m4.x, m4.y, m4.z, m4.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        d = fmaf(bf16_lo(a[e]) - bf16_lo(b[e]), bf16_lo(h[e]) - bf16_lo(m[e]), d);
-                        d = fmaf(bf16_hi(a[e]) - bf16_hi(b[e]), bf16_hi(h[e]) - bf16_hi(m[e]), d);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const float4 y = *state_of(i);
+                    d = fmaf(x[i].x, y.x, d), d = fmaf(x[i].y, y.y, d), d = fmaf(x[i].z, y.z, d), d = fmaf(x[i].w, y.w, d);
+                    x[i] = y;
                 }
+                grad_sync();
+                put_two(x, third);
+                grad_arrive<6>();
                 for (int o = 16; o > 0; o /= 2) d += __shfl_xor_sync(0xffffffffu, d, o);
                 if (l.g == 0 && l.c == 0) sm.ds[warp] = d;
             }
-            grad_arrive<4>();
             failed = failed || !wait_products(&bar_out, turn);
+            put_third(sm.r[0], third);  // (p and m are used up)
+            grad_arrive<4>();
+            tc_fence_after_sync();
+#pragma unroll
+            for (int lh = 0; lh < 2; ++lh) {
+                float a[8], b[8];
+                tm_ld16(lanes + (lh << 20) + kTmDQ, a);
+                tm_ld16(lanes + (lh << 20) + kTmDK, b);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dq[lh][i] += a[i], dk[lh][i] += b[i];
+            }
             failed = failed || !wait_products(&bar_d, turn);
             tc_fence_after_sync();
 #pragma unroll
             for (int lh = 0; lh < 2; ++lh) {
-                float a[8], b[8], y[8];
-                tm_ld16(lanes + (lh << 20) + kTmDQ, a);
-                tm_ld16(lanes + (lh << 20) + kTmDK, b);
+                float y[8];
                 tm_ld16(lanes + (lh << 20) + kTmUD, y);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    dq[lh][i] += a[i];
-                    dk[lh][i] += fmaf(sm.tab[TAB_ECK * kC + t0 + i / 4 * 8 + i % 2], y[i], b[i]);
-                }
+                for (int i = 0; i < 8; ++i) dk[lh][i] = fmaf(sm.tab[TAB_ECK * kC + t0 + i / 4 * 8 + i % 2], y[i], dk[lh][i]);
             }
             tc_fence_before_sync();
             if (!last) {

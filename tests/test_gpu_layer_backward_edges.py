@@ -33,3 +33,45 @@ def test_decays_are_accurate_to_their_own_size(B, T, H_k, H_v):
         t = got[NAMES.index(n)].reshape(ref[n].shape).double()
         err = ((t - ref[n]).norm() / ref[n].norm()).item()
         assert err <= tol, (n, err)
+
+
+# 1 + 2^-9 + 0.9 x 2^-17: of two bf16 pieces 1 and 2^-9 stay, off by 6.9e-6
+HARD = 1 + 2.0 ** -9 + 0.9 * 2.0 ** -17
+
+
+def test_states_count_with_all_their_bits_in_dg():
+    """One token with beta = 0 and values of one sign. dg = exp(g) <D, S>: 32 products in a row, 5 and 16 sums, exp: (32 + 21 + 4) x 2^-24. Without D,
+    scale exp(g) <q, S^T dO>: 24 accumulations of 2^-23 each, 11 + 10 additions, exp and rsqrt."""
+    x = _inputs(1, 1, 1, 51)
+    x["beta"].zero_()
+    x["g"].fill_(-0.5)
+    x["S"].fill_(HARD)
+    x["dS"].fill_(HARD)
+    x["Q"].fill_(1)
+    x["dO"].zero_()
+    dg = _call(_dense(x, 1, 1), x)[4].double().item()
+    ref = torch.tensor(-0.5, dtype=torch.float64).exp().item() * D * D * x["S"].double()[0, 0, 0, 0].item() ** 2
+    assert abs(dg / ref - 1) <= 57 * 2 ** -24, dg / ref - 1
+    x["dS"].zero_()
+    x["dO"].fill_(1)
+    dg = _call(_dense(x, 1, 1), x)[4].double().item()
+    ref = D ** -0.5 * torch.tensor(-0.5, dtype=torch.float64).exp().item() * D * D ** 0.5 * x["S"].double()[0, 0, 0, 0].item()
+    assert abs(dg / ref - 1) <= (48 + 21 + 8) * 2 ** -24, dg / ref - 1
+
+
+def test_bf16_gradients_are_rounded_once():
+    """dQ of single tokens with beta = 0, dq = scale exp(g) S^T dO, against the fp64 value's own rounding to bf16: they differ where a border between two bf16
+    values lies between the exact value and the kernel's, whose share is the error over the distance of the borders. States of one sign: off by 77 x 2^-24
+    at most (see above), borders 2^-7 to 2^-8 of the value apart, 1.4 x 2^-8 on the average of the reciprocals over a mantissa: less than 77 x 2^-24 x 2^8 / 1.4
+    = 8.4e-4. Two pieces of a state that is HARD times powers of two are 6.9e-6 off, which gives 1.3e-3 of 262144 values: 5e-4 more, by a scatter of 7e-5."""
+    B, H = 128, 16
+    x = _inputs(B, H, H, 52, B)
+    x["g"].fill_(-0.5)
+    x["beta"].zero_()
+    gen = torch.Generator(device="cuda").manual_seed(53)
+    x["S"] = HARD * 2.0 ** torch.randint(0, 4, x["S"].shape, generator=gen, device="cuda").float()
+    x["dO"] = x["dO"].float().abs().bfloat16()
+    got = _call(_dense(x, B, 1), x, qk_l2norm=False, with_dS=False)
+    ref = D ** -0.5 * x["g"].double().exp()[..., None] * torch.einsum("bhvk,bhv->bhk", x["S"].double(), x["dO"].double())
+    share = (got[0].reshape(ref.shape) != ref.bfloat16()).double().mean().item()
+    assert share <= 8.4e-4, share
