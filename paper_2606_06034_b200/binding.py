@@ -655,7 +655,8 @@ def gated_delta_step(Q, K, V, beta, g_raw, S, slots=None, scale=None, *, token_m
 def gated_delta_layer_backward(dO, Q, K, V, beta, g_raw, C=64, scale=None, S_in=None, dS_out=None, *, cu_seqlens=None, token_major=True,
                                qk_l2norm=True, workspace=None):
     """Gradients of `gated_delta_layer` with the same arguments: dO like V (the gradient of O) and, where the final states went
-    into the loss, dS_out [B or n_seq,H_v,d_v,d_k] fp32. Any T. bf16, C = 64, d = 128. Nothing has to be kept from the forward pass.
+    into the loss, dS_out [B or n_seq,H_v,d_v,d_k] fp32. bf16, C = 64, d = 128. Any T, like the packed forward call (the dense forward one takes
+    multiples of C: what belongs to other lengths is the packed call with cu_seqlens = [0, T, ...]). Nothing has to be kept from the forward pass.
     workspace: a uint8 CUDA tensor of gdn_gated_delta_layer_backward_workspace bytes to reuse between calls (default: allocated).
     Returns (dQ, dK, dV, dbeta, dg_raw, dS_in), dS_in None without an S_in. Rows that no packed sequence covers get zeros."""
     where = "gated_delta_layer_backward"

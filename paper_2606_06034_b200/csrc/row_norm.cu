@@ -383,8 +383,11 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, in
     }
 }
 
-// Threads that a launch brings per SM, at most: as many as are resident there (80 registers backward, 48 forward), so that no CTA is left for a second
-// round. 1 M rows of 128 (with the sigmoid as it was): backward 0.264 ms, with 1024 threads 0.314; forward 0.147, with 1024 0.156, with 1536 0.176.
+// Threads that a launch brings per SM, at most: as many as are resident there (80 registers backward, 48 forward) of bf16 rows in whole vectors with one
+// vector a thread (up to 256 features and from 513 to 2048), so that no CTA is left for a second round. 1 M rows of 128 (with the sigmoid as it was):
+// backward 0.264 ms, with 1024 threads 0.314; forward 0.147, with 1024 0.156, with 1536 0.176. The other instantiations take more registers and the rule
+// was not measured for them: some CTAs of theirs come in a second round (resident / launched per SM, backward: fp32 2 / 3 up to 256 features, 1 / 3 to
+// 512, 3 or 4 / 6 to 1024, 1 or 2 / 3 to 2048, bf16 1 / 3 from 257 to 512; forward: fp32 3 or 4 / 5 up to 256, 2 / 5 to 512, 1 / 2 above 4096).
 constexpr int kForwardThreads = 1280, kBackwardThreads = 768;
 
 // threads of a row; CTAs of a launch
