@@ -33,3 +33,19 @@ def test_outputs_that_lie_on_inputs():
     assert gdn.gated_delta_step(Q, K, V, beta, g, S, out=V) is V
     _near(V, ref[0], TOL[torch.bfloat16])
     _near(S, ref[1], TOL[torch.float32])
+
+
+def test_a_twin_more_than_one_cta_of_rows_away():
+    B, n = 700, 800
+    Q, K, V, beta, g, S = _inputs(B, 1, 1, 1, 128, 128, torch.bfloat16, 7, n_slots=n)
+    slots = torch.randperm(n, generator=torch.Generator().manual_seed(8))[:B].int()
+    slots[650], slots[699], slots[300] = slots[3], slots[400], -1
+    before = S.clone()
+    ref = _expected(Q, K, V, beta, g, S, [(b, int(s)) for b, s in enumerate(slots) if b not in (650, 699, 300)])
+    O = gdn.gated_delta_step(Q, K, V, beta, g, S, slots.cuda())
+    assert gdn.gdn_device_status() == gdn.GDN_ERR_INVALID_ARG
+    assert not O[650].any() and not O[699].any() and not O[300].any()
+    _near(O, ref[0], TOL[torch.bfloat16])
+    _near(S, ref[1], TOL[torch.float32])
+    left = sorted(set(range(n)) - set(slots.tolist()))
+    assert torch.equal(S[left], before[left])
