@@ -35,9 +35,9 @@ def test_no_rows_and_no_workspace():
 @pytest.mark.parametrize("width", [128, 75, 2048])
 def test_gates_far_below_zero_keep_fp32_rows_exact(width):
     """y and dgate of fp32 rows, value by value, where silu is small: z from -85 to -40. The rows hold 1 and -1 and their RMS is 1, so no sum is rounded. Off
-    by at most, in steps of 2^-24: rsqrt 4, exp(-z) 2 (its sum with 1 and the quotient 2), three products 3: 11, and 12 for second order. dgate: the slope
-    s + z s (1 - s) is z s less a fortieth at most, s is off by 4, the product and the sum by 2, both times 41 / 39; rsqrt 4, products 3: 14, doubled for
-    a margin that an exponent rounded before exp is taken does not fit into (|z| log2(e) = 123, off by 2^-18, is 44 steps by itself, and log2(e) in fp32 17)."""
+    by at most, in steps of 2^-24: rsqrt 4, exp(-z) 2, its sum with 1 1, the reciprocal 2, three products 3: 12. dgate: the slope s + z s (1 - s) is z s less a
+    fortieth at most, s is off by 5, the product and the sum by 2, both times 41 / 39; rsqrt 4, products 3: 15; 28 leaves a margin into which an exponent
+    rounded before exp is taken does not fit (|z| log2(e) = 123, off by 2^-18, is 44 steps by itself, and log2(e) in fp32 17)."""
     gen = torch.Generator().manual_seed(width)
     z = (-85 + 45 * torch.rand(64, width, generator=gen)).cuda()
     x = torch.where(torch.rand(64, width, generator=gen) < 0.5, -1.0, 1.0).cuda()  # (rms: n = x, no sum is rounded)
