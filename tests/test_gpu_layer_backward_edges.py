@@ -75,3 +75,17 @@ def test_bf16_gradients_are_rounded_once():
     ref = D ** -0.5 * x["g"].double().exp()[..., None] * torch.einsum("bhvk,bhv->bhk", x["S"].double(), x["dO"].double())
     share = (got[0].reshape(ref.shape) != ref.bfloat16()).double().mean().item()
     assert share <= 8.4e-4, share
+
+
+def test_gradient_of_the_state_in_the_place_of_the_next_ones():
+    """dS_in may be dS_out: the gradients of a text's pieces are handed down in one tensor."""
+    T, n = 200, 2
+    x = _inputs(T, 1, 2, 54, n)
+    cu = torch.tensor([0, 70, T], dtype=torch.int32, device="cuda")
+    ref = _call(x, x, cu_seqlens=[0, 70, T])
+    outs = [torch.empty_like(x[k]) for k in NAMES]
+    ws = torch.empty(gdn.gdn_gated_delta_layer_backward_workspace(n, T, 2), dtype=torch.uint8, device="cuda")
+    flags = gdn.GDN_FLAG_G_RAW | gdn.GDN_FLAG_LAYOUT_BTHD | gdn.GDN_FLAG_K_L2NORM
+    gdn.gdn_gated_delta_layer_backward_varlen(x["dO"], *(x[k] for k in NAMES), cu, n, T, 1, 2, 64, D, D, D ** -0.5, x["S"], x["dS"], *outs, x["dS"], ws, flags)
+    assert gdn.gdn_device_status() == gdn.GDN_OK
+    assert all(torch.equal(p, q) for p, q in zip([*outs, x["dS"]], ref))

@@ -24,11 +24,8 @@ def _step(lib, **kw):
                                   gdn.GDN_FLAG_LAYOUT_BTHD, None)
 
 
-@pytest.mark.parametrize("out", ["O", "S"])
-@pytest.mark.parametrize("other", ["Q", "K", "V", "beta", "g", "slots", "S"])
+@pytest.mark.parametrize("out,other", [("O", "S")] + [(out, other) for out in ("O", "S") for other in ("Q", "K", "V", "beta", "g", "slots")])
 def test_one_byte_in_common_is_refused(lib, out, other):
-    if out == other:
-        pytest.skip("the same tensor")
     up = (SIZE[other] + 15) // 16 * 16  # the first 16-byte boundary behind the other one
     for at in (AT[other] + up - 16, AT[other] - SIZE[out] + 16):
         assert _step(lib, **{out: at}) == gdn.GDN_ERR_INVALID_ARG
