@@ -378,7 +378,8 @@ size_t gdn_gated_delta_layer_backward_workspace(int n_seq, long long tokens, int
  *     n = (x - mean(x)) / sqrt(var(x) + eps)      (GDN_NORM_RMS: n = x / sqrt(mean(x^2) + eps))
  *     y = (n * weight + bias) * gate * sigmoid(gate)
  *   x, gate, y [rows,width], contiguous, fp32 or bf16 (`dtype`); weight, bias [width], fp32 or bf16 (`param_dtype`); weight, bias
- *   and gate may each be NULL (1, 0, and no gate). y may be x or gate. 1 <= width <= 16384. Statistics and arithmetic in fp32.
+ *   and gate may each be NULL (1, 0, and no gate). y may be x or gate, otherwise nothing that is written may overlap another argument
+ *   (GDN_ERR_INVALID_ARG where rows do). 1 <= width <= 16384. Statistics and arithmetic in fp32.
  * Backward: dx, dgate like x (dgate exactly where there is a gate), dweight, dbias [width] fp32: sums over the rows, accumulated in fp32 in an
  *   order that depends on the shape alone; required where there is a weight / a bias, NULL otherwise. dx may be dy or x, dgate may be gate.
  *   workspace: DEVICE memory of gdn_layer_norm_backward_workspace(rows, width) bytes, 16-byte aligned (needed for dweight or dbias).

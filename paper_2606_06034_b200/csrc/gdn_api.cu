@@ -399,6 +399,16 @@ static int layer_norm(const ProblemN& q, bool backward, size_t workspace_bytes, 
     for (const void* x : {q.dy, q.x, q.weight, q.bias, q.gate, static_cast<const void*>(q.y), static_cast<const void*>(q.dx), static_cast<const void*>(q.dgate),
                           static_cast<const void*>(q.dweight), static_cast<const void*>(q.dbias), static_cast<const void*>(q.workspace)})
         if (!aligned16(x)) return GDN_ERR_ALIGN;
+    // rows are stored while others are still read: in place is in the same place
+    const long long rows = q.rows * q.width * (q.dtype == GDN_DTYPE_BF16 ? 2 : 4), params = static_cast<long long>(q.width) * (q.param_dtype == GDN_DTYPE_BF16 ? 2 : 4);
+    for (const void* out : {static_cast<const void*>(q.y), static_cast<const void*>(q.dx), static_cast<const void*>(q.dgate)}) {
+        if (out == nullptr) continue;
+        for (const void* in : {q.x, q.gate, q.dy})
+            if (in != nullptr && in != out && overlap(out, rows, in, rows)) return GDN_ERR_INVALID_ARG;
+        for (const void* in : {q.weight, q.bias})
+            if (in != nullptr && overlap(out, rows, in, params)) return GDN_ERR_INVALID_ARG;
+    }
+    if (q.dgate != nullptr && overlap(q.dx, rows, q.dgate, rows)) return GDN_ERR_INVALID_ARG;
     const int rc = check_arch();
     return rc != GDN_OK ? rc : launch_layer_norm(q, backward, static_cast<cudaStream_t>(stream));
 }

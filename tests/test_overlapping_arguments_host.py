@@ -1,4 +1,4 @@
-"""The decoding step refuses outputs that lie on what other threads still read. No GPU needed: every call here is refused before the device is asked for."""
+"""The decoding step and the norms refuse outputs that lie on what other threads still read. No GPU needed: every call here is refused before the device is asked for."""
 import pytest
 
 from paper_2606_06034_b200 import binding as gdn
@@ -33,3 +33,32 @@ def test_one_byte_in_common_is_refused(lib, out, other):
 
 def test_v_that_is_q_too_may_not_be_written_over(lib):
     assert _step(lib, O=AT["V"], Q=AT["V"]) == gdn.GDN_ERR_INVALID_ARG
+
+
+ROWS, W = 64, 256
+X = {n: (i + 1) * 16 * MB for i, n in enumerate(("dy", "x", "weight", "bias", "gate", "out", "dgate", "dweight", "dbias", "ws"))}
+BYTES = ROWS * W * 2
+
+
+def _norm(lib, backward, **kw):
+    a = {**X, **kw}
+    if backward:
+        return lib.gdn_layer_norm_backward(a["dy"], a["x"], a["weight"], a["bias"], a["gate"], ROWS, W, 1e-5, gdn.GDN_DTYPE_BF16, gdn.GDN_DTYPE_FP32, a["out"], a["dweight"], a["dbias"],
+                                           a["dgate"], a["ws"], 1 << 30, 0, None)
+    return lib.gdn_layer_norm(a["x"], a["weight"], a["bias"], a["gate"], ROWS, W, 1e-5, gdn.GDN_DTYPE_BF16, gdn.GDN_DTYPE_FP32, a["out"], 0, None)
+
+
+@pytest.mark.parametrize("backward,out,other", [(False, "out", n) for n in ("x", "gate")] + [(True, out, n) for out in ("out", "dgate") for n in ("dy", "x", "gate")])
+def test_rows_that_are_moved_are_refused(lib, backward, out, other):
+    for by in (16, W * 2, BYTES - 16, -16, 16 - BYTES):
+        assert _norm(lib, backward, **{out: X[other] + by}) == gdn.GDN_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("backward,out", [(False, "out"), (True, "out"), (True, "dgate")])
+def test_rows_on_parameters_or_on_each_other_are_refused(lib, backward, out):
+    for other in ("weight", "bias"):
+        for by in (0, W * 4 - 16, 16 - BYTES):
+            assert _norm(lib, backward, **{out: X[other] + by}) == gdn.GDN_ERR_INVALID_ARG
+    if backward:
+        assert _norm(lib, True, out=X["dgate"] + 32) == gdn.GDN_ERR_INVALID_ARG
+        assert _norm(lib, True, out=X["dgate"]) == gdn.GDN_ERR_INVALID_ARG
